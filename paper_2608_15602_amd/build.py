@@ -2,7 +2,7 @@
 
 Usage: python -m paper_2608_15602_amd.build [--jobs N] [--host-sanitizers]
 The shared library lands next to this file, where the Python binding loads it from. --host-sanitizers also builds
-libfluxbin_hostsan.so: the same library with its host code (fluxbin_host.cpp: validation, sizes, launch planning,
+libfluxbin_hostsan.so: the same library with its host code (HOST_SOURCES: validation, sizes, launch planning,
 headers) instrumented by AddressSanitizer and UndefinedBehaviorSanitizer, for CPU-only tests (the device code is the
 ordinary build's; no sanitizer touches GPU code).
 """
@@ -29,7 +29,8 @@ SAN_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=und
 SOURCES = ["fluxbin_host.cpp", "fluxbin_pack.hip", "fluxbin_gemv.hip", "fluxbin_gemm_batch.hip",
            "fluxbin_gemm_mfma.hip", "fluxbin_rc.hip", "fluxbin_noalloc.hip",
            "fluxbin_gemv_rows.hip", "fluxbin_gemm_mfma_rows.hip", "fluxbin_gemm_mx.hip",
-           "fluxbin_gemm_prefill.hip"]
+           "fluxbin_gemm_prefill.hip", "fluxbin_quant_host.cpp", "fluxbin_w4.hip"]
+HOST_SOURCES = ("fluxbin_host.cpp", "fluxbin_quant_host.cpp")   # what --host-sanitizers instruments
 ARCH = "gfx950"
 
 # Packed-FP32 instructions are kept out of the generated code (plain float code only).
@@ -81,14 +82,14 @@ def asan_runtime() -> str:
 
 
 def build_host_sanitized(verbose: bool = True) -> str:
-    """libfluxbin_hostsan.so: fluxbin_host.cpp compiled with host ASan + UBSan, linked with the device objects of the
+    """libfluxbin_hostsan.so: the host sources compiled with host ASan + UBSan, linked with the device objects of the
     ordinary build (built first if missing)."""
     os.makedirs(OBJDIR, exist_ok=True)
     objs = []
     for src in SOURCES:
         obj = os.path.join(OBJDIR, os.path.basename(src) + ".o")
-        if src == "fluxbin_host.cpp":
-            obj = os.path.join(OBJDIR, "fluxbin_host_san.o")
+        if src in HOST_SOURCES:
+            obj = os.path.join(OBJDIR, src[:-len(".cpp")] + "_san.o")
             cmd = [hipcc()] + COMMON + SAN_FLAGS + ["-c", os.path.join(CSRC, src), "-o", obj]
             r = subprocess.run(cmd, capture_output=True, text=True)
             if r.returncode != 0:

@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libfluxbin (include/fluxbin.h): argument marshalling only.
+"""Thin ctypes binding of libfluxbin (include/fluxbin.h, include/fluxbin_quant.h): argument marshalling only.
 
 Every step of the hot path runs in the library's HIP kernels; PyTorch only provides device memory and the stream.
 The functions keep the C names. Tensors must be on the current CUDA (HIP) device unless stated otherwise.
@@ -28,6 +28,10 @@ EXPORTS = (
     "fluxbin_lut_gemm_smallbatch", "fluxbin_debug_indices", "fluxbin_unpack_canonical", "fluxbin_stream_probe",
     "fluxbin_rc_workspace_query", "fluxbin_rc_decompose", "fluxbin_structural_search", "fluxbin_get_tuning",
     "fluxbin_set_tuning", "fluxbin_plan_query", "fluxbin_lut_gemv_noalloc",
+)
+# Entry points declared in include/fluxbin_quant.h.
+QUANT_EXPORTS = (
+    "fluxbin_w4_quantize", "fluxbin_w4_pack_query", "fluxbin_w4_pack", "fluxbin_w4_workspace_query", "fluxbin_w4_gemm",
 )
 NOALLOC_SCRATCH_BYTES = 8 << 20
 
@@ -59,6 +63,16 @@ class Layer(ctypes.Structure):
                 ("Mp", ctypes.c_int64), ("Gr", ctypes.c_int64), ("Gs", ctypes.c_int64), ("NRP", ctypes.c_int64),
                 ("off_signs", ctypes.c_uint64), ("off_rscale", ctypes.c_uint64), ("off_colscale", ctypes.c_uint64),
                 ("off_xidx", ctypes.c_uint64), ("off_chunk_plane", ctypes.c_uint64), ("off_sal_idx", ctypes.c_uint64)]
+
+
+class W4Shape(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int64), ("g", ctypes.c_int64), ("has_zeros", ctypes.c_int32),
+                ("reserved0", ctypes.c_int32)]
+
+
+class W4Layer(ctypes.Structure):
+    _fields_ = [("shape", W4Shape), ("d_base", ctypes.c_void_p), ("bytes", ctypes.c_uint64),
+                ("format_version", ctypes.c_uint32), ("reserved1", ctypes.c_uint32)]
 
 
 class Tuning(ctypes.Structure):
@@ -110,7 +124,12 @@ def lib() -> ctypes.CDLL:
         L.fluxbin_set_tuning.argtypes = [ctypes.POINTER(Tuning)]
         L.fluxbin_plan_query.argtypes = [ctypes.POINTER(Layer), i32, ctypes.POINTER(PlanInfo)]
         L.fluxbin_lut_gemv_noalloc.argtypes = [ctypes.POINTER(Layer), vp, vp, i32, vp]
-        for name in EXPORTS:
+        L.fluxbin_w4_quantize.argtypes = [ctypes.POINTER(W4Shape), vp, i32, i64, vp, vp, vp, vp, i64, vp]
+        L.fluxbin_w4_pack_query.argtypes = [ctypes.POINTER(W4Shape), ctypes.POINTER(sz)]
+        L.fluxbin_w4_pack.argtypes = [ctypes.POINTER(W4Shape), vp, vp, vp, vp, sz, ctypes.POINTER(W4Layer), vp]
+        L.fluxbin_w4_workspace_query.argtypes = [ctypes.POINTER(W4Layer), i32, ctypes.POINTER(sz)]
+        L.fluxbin_w4_gemm.argtypes = [ctypes.POINTER(W4Layer), i32, vp, i64, vp, i64, i32, vp, sz, vp]
+        for name in EXPORTS + QUANT_EXPORTS:
             if name not in ("fluxbin_status_string", "fluxbin_last_error_message"):
                 getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -331,6 +350,128 @@ def fluxbin_structural_search(W, hinv_diag, g: int, s: int, stream=None):
                                            scores.data_ptr(), idx.data_ptr(), mask.data_ptr(), _stream(stream)))
     return scores, idx, mask
 
+
+# ---- linears in 4 bits with group scales ----
+
+def _invalid(message: str) -> FluxbinError:
+    return FluxbinError(FLUXBIN_ERR_INVALID_ARG, message)
+
+
+def _on_device(device, **tensors) -> None:
+    """Launches go to the current device: it must be the operands'."""
+    import torch
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise _invalid(f"operands are on {device}, which is not the current CUDA (HIP) device")
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise _invalid(f"{name} is on {t.device}, not on {device}")
+
+
+def _dense(name: str, t, dtype, shape) -> None:
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise _invalid(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} "
+                       f"{tuple(t.shape)}")
+
+
+def fluxbin_w4_quantize(W, g: int, asymmetric: bool = True, values: bool = False, stream=None):
+    """Round-to-nearest 4-bit quantization of W (fp16 or fp32 [M, N], unit inner stride) with one scale per row and group of
+    g columns, and a zero point where asymmetric. Returns (codes int32 [M, ceil(N/8)], scales fp16 [M, G], zeros uint8
+    [M, G] or None, the values the codes stand for as fp16 [M, N] with values, else None)."""
+    import torch
+    if W.dim() != 2 or W.dtype not in (torch.float16, torch.float32) or (W.shape[1] > 1 and W.stride(1) != 1):
+        raise _invalid("W must be fp16 or fp32 [M, N] with unit inner stride")
+    _on_device(W.device)
+    M, N = W.shape
+    if g < 1:
+        raise _invalid(f"g = {g} must be >= 1")
+    G = -(-N // g)
+    new = lambda dtype, *size: torch.empty(size, dtype=dtype, device=W.device)
+    codes, scales = new(torch.int32, M, -(-N // 8)), new(torch.float16, M, G)
+    zeros = new(torch.uint8, M, G) if asymmetric else None
+    out = new(torch.float16, M, N) if values else None
+    shape = W4Shape(M, N, int(g), 1 if asymmetric else 0, 0)
+    _check(lib().fluxbin_w4_quantize(ctypes.byref(shape), W.data_ptr(), 1 if W.dtype == torch.float32 else 0,
+                                     max(N, W.stride(0)) if M == 1 else W.stride(0), codes.data_ptr(), scales.data_ptr(),
+                                     _ptr(zeros), _ptr(out), N, _stream(stream)))
+    return codes, scales, zeros, out
+
+
+class PackedW4:
+    """A packed 4-bit layer: its device buffer (torch uint8 tensor) and C descriptor."""
+
+    def __init__(self, buf, layer: W4Layer):
+        self.buf = buf
+        self.layer = layer
+        self.M, self.N, self.device, self.ref = layer.shape.M, layer.shape.N, buf.device, ctypes.byref(layer)
+
+    @property
+    def shape(self) -> W4Shape:
+        return self.layer.shape
+
+
+def fluxbin_w4_pack_query(shape: W4Shape) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().fluxbin_w4_pack_query(ctypes.byref(shape), ctypes.byref(n)))
+    return n.value
+
+
+def fluxbin_w4_pack(codes, scales, zeros, N: int, g: int, stream=None) -> PackedW4:
+    """Pack codes, scales and zero points (None: 8 everywhere) as fluxbin_w4_quantize returns them."""
+    import torch
+    if codes.dim() != 2 or g < 1 or N < 1:
+        raise _invalid("codes must be int32 [M, ceil(N/8)], N and g at least 1")
+    M, G = codes.shape[0], -(-N // g)
+    _on_device(codes.device, scales=scales, zeros=zeros)
+    _dense("codes", codes, torch.int32, (M, -(-N // 8)))
+    _dense("scales", scales, torch.float16, (M, G))
+    if zeros is not None:
+        _dense("zeros", zeros, torch.uint8, (M, G))
+    shape = W4Shape(M, int(N), int(g), 0 if zeros is None else 1, 0)
+    n = fluxbin_w4_pack_query(shape)
+    buf = torch.empty(n, dtype=torch.uint8, device=codes.device)
+    out = W4Layer()
+    _check(lib().fluxbin_w4_pack(ctypes.byref(shape), codes.data_ptr(), scales.data_ptr(), _ptr(zeros), buf.data_ptr(), n,
+                                 ctypes.byref(out), _stream(stream)))
+    return PackedW4(buf, out)
+
+
+def fluxbin_w4_workspace_query(layer: PackedW4, B: int = 1) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().fluxbin_w4_workspace_query(layer.ref, int(B), ctypes.byref(n)))
+    return n.value
+
+
+def make_w4_workspace(layer: PackedW4, B: int = 1):
+    """A workspace (torch uint8 tensor, nothing to clear) for calls of up to B rows."""
+    import torch
+    return torch.empty(max(256, fluxbin_w4_workspace_query(layer, B)), dtype=torch.uint8, device=layer.device)
+
+
+def fluxbin_w4_gemm(layer: PackedW4, x, y=None, out_fp32: bool = False, workspace=None, stream=None):
+    """y = What x: x fp16 [N] or [B, N] with unit inner stride, y [M] or [B, M]."""
+    import torch
+    M, N, dev = layer.M, layer.N, layer.device
+    dtype = torch.float32 if out_fp32 else torch.float16
+    one = x.dim() == 1
+    B = 1 if one else x.shape[0]
+    if y is None:
+        y = torch.empty(M if one else (B, M), dtype=dtype, device=x.device)
+    if x.dtype != torch.float16 or x.device != dev or tuple(x.shape) != ((N,) if one else (B, N)) or \
+            (N > 1 and x.stride(-1) != 1):
+        raise _invalid(f"x must be fp16 [{N}] or [B, {N}] on {dev} with unit inner stride, got {x.dtype} {tuple(x.shape)}")
+    if y.dtype != dtype or y.device != dev or tuple(y.shape) != ((M,) if one else (B, M)) or (M > 1 and y.stride(-1) != 1):
+        raise _invalid(f"y must be {dtype} {[M] if one else [B, M]} on {dev} with unit inner stride, got {y.dtype} "
+                       f"{tuple(y.shape)}")
+    if dev.index != torch.cuda.current_device():
+        raise _invalid(f"operands are on {dev}, which is not the current CUDA (HIP) device")
+    if workspace is None:
+        workspace = make_w4_workspace(layer, B)
+    elif workspace.device != dev:
+        raise _invalid(f"workspace is on {workspace.device}, not on {dev}")
+    _check(lib().fluxbin_w4_gemm(layer.ref, B, x.data_ptr(), 0 if B == 1 else x.stride(0), y.data_ptr(),
+                                 0 if B == 1 else y.stride(0), 1 if out_fp32 else 0, workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), _stream(stream)))
+    return y
 
 
 def fluxbin_get_tuning() -> Dict[str, int]:

@@ -1,0 +1,134 @@
+"""Host-side checks of include/fluxbin_quant.h: entry points, sizes and refusals, before any launch. CPU only."""
+import ctypes
+import os
+import re
+
+import pytest
+
+fb = pytest.importorskip("paper_2608_15602_amd.fluxbin")
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+INV, UNS, SMALL = fb.FLUXBIN_ERR_INVALID_ARG, fb.FLUXBIN_ERR_UNSUPPORTED, fb.FLUXBIN_ERR_BUFFER_TOO_SMALL
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(fb.LIB_PATH):
+        pytest.fail("libfluxbin.so is not built; run `python -m paper_2608_15602_amd.build`")
+    return fb.lib()
+
+
+def test_exports_every_declared_function(L):
+    with open(os.path.join(ROOT, "include", "fluxbin_quant.h")) as f:
+        names = set(re.findall(r"^fluxbin_status (fluxbin_\w+)\(", f.read(), re.M))
+    assert names == set(fb.QUANT_EXPORTS)
+    for n in names:
+        assert hasattr(L, n), n
+
+
+def _w4(**kw):
+    d = dict(M=300, N=1000, g=128, has_zeros=1)
+    d.update(kw)
+    return fb.W4Shape(d["M"], d["N"], d["g"], d["has_zeros"], 0)
+
+
+def _up(n):
+    return -(-n // 256) * 256
+
+
+@pytest.mark.parametrize("kw", [{}, dict(M=1, N=1, g=1), dict(g=32), dict(g=64, has_zeros=0), dict(N=129, g=5000),
+                                dict(M=28672, N=8192), dict(N=1 << 20, M=1 << 14, g=256)])
+def test_w4_pack_query(L, kw):
+    s = _w4(**kw)
+    Mt, Nc = -(-s.M // 16), -(-s.N // 128)
+    gc = 128 // s.g if s.g < 128 and s.g < s.N else 1
+    Nq = -(-Nc * gc // 4)
+    assert fb.fluxbin_w4_pack_query(s) == _up(Mt * Nc * 1024) + _up(Mt * Nq * 128) + (_up(Mt * Nq * 64) if s.has_zeros else 0)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(M=0), INV), (dict(M=-1), INV), (dict(M=(1 << 24) + 1), INV), (dict(N=0), INV), (dict(N=(1 << 20) + 1), INV),
+    (dict(M=1 << 24, N=1025), UNS), (dict(g=0), INV), (dict(g=-128), INV), (dict(g=16), UNS), (dict(g=96), UNS),
+    (dict(g=200), UNS), (dict(has_zeros=2), INV)])
+def test_w4_shape_refused(L, kw, status):
+    n = ctypes.c_size_t(7)
+    assert L.fluxbin_w4_pack_query(ctypes.byref(_w4(**kw)), ctypes.byref(n)) == status
+    assert L.fluxbin_last_error_message() and n.value == 7
+
+
+def test_w4_null_pointers(L):
+    s, n = _w4(), ctypes.c_size_t(0)
+    assert L.fluxbin_w4_pack_query(None, ctypes.byref(n)) == INV
+    assert L.fluxbin_w4_pack_query(ctypes.byref(s), None) == INV
+    assert L.fluxbin_w4_workspace_query(None, 1, ctypes.byref(n)) == INV
+
+
+A = [1 << 20, 2 << 20, 4 << 20, 6 << 20, 8 << 20]   # addresses for calls that are refused before any launch
+
+
+def _quantize(L, **kw):
+    a = dict(shape=_w4(), W=A[0], fp32=0, ldw=1000, codes=A[1], scales=A[2], zeros=A[3], values=None, ldv=0)
+    a.update(kw)
+    return L.fluxbin_w4_quantize(ctypes.byref(a["shape"]), a["W"], a["fp32"], a["ldw"], a["codes"], a["scales"], a["zeros"],
+                                 a["values"], a["ldv"], None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(W=None), INV), (dict(codes=None), INV), (dict(scales=None), INV), (dict(zeros=None), INV),
+    (dict(shape=_w4(has_zeros=0)), INV), (dict(fp32=2), INV), (dict(ldw=999), INV), (dict(ldw=-1000), INV),
+    (dict(W=A[0] + 1), INV), (dict(W=A[0] + 2, fp32=1), INV), (dict(codes=A[1] + 2), INV), (dict(scales=A[2] + 1), INV),
+    (dict(values=A[4], ldv=999), INV), (dict(values=A[4] + 1, ldv=1000), INV), (dict(codes=A[0] + 4), INV),
+    (dict(scales=A[1] + 8), INV), (dict(zeros=A[2] + 2), INV), (dict(values=A[0] + 300 * 2000 - 2, ldv=1000), INV),
+    (dict(shape=_w4(g=48)), UNS)])
+def test_w4_quantize_refused(L, kw, status):
+    assert _quantize(L, **kw) == status
+    assert L.fluxbin_last_error_message()
+
+
+def _pack(L, **kw):
+    s = kw.pop("shape", _w4())
+    a = dict(codes=A[0], scales=A[1], zeros=A[2], packed=A[3], bytes=1 << 20)
+    a.update(kw)
+    out = fb.W4Layer()
+    return L.fluxbin_w4_pack(ctypes.byref(s), a["codes"], a["scales"], a["zeros"], a["packed"], a["bytes"],
+                             ctypes.byref(out), None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(codes=None), INV), (dict(scales=None), INV), (dict(zeros=None), INV), (dict(packed=None), INV),
+    (dict(shape=_w4(has_zeros=0)), INV), (dict(bytes=1000), SMALL), (dict(packed=A[3] + 8), INV), (dict(codes=A[0] + 1), INV),
+    (dict(packed=A[0] + 16), INV), (dict(zeros=A[3] + 64), INV)])
+def test_w4_pack_refused(L, kw, status):
+    assert _pack(L, **kw) == status
+
+
+def _layer(**kw):
+    layer = fb.W4Layer(_w4(**kw.pop("shape", {})), A[0], 1 << 20, 1, 0)
+    for k, v in kw.items():
+        setattr(layer, k, v)
+    return layer
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(layer=dict(format_version=2)), INV), (dict(layer=dict(d_base=None)), INV), (dict(layer=dict(bytes=1000)), SMALL),
+    (dict(layer=dict(d_base=A[0] + 4)), INV), (dict(layer=dict(shape=dict(g=48))), UNS), (dict(B=0), INV), (dict(B=8193), INV),
+    (dict(x=None), INV), (dict(y=None), INV), (dict(fp32=3), INV), (dict(B=2, ldx=999), INV), (dict(B=2, ldy=299), INV),
+    (dict(x=A[2] + 1), INV), (dict(y=A[3] + 2, fp32=1), INV)])
+def test_w4_gemm_refused(L, kw, status):
+    a = dict(layer={}, B=1, x=A[2], ldx=1000, y=A[3], ldy=300, fp32=0, ws=A[4], bytes=1 << 20)
+    a.update(kw)
+    assert L.fluxbin_w4_gemm(ctypes.byref(_layer(**a["layer"])), a["B"], a["x"], a["ldx"], a["y"], a["ldy"], a["fp32"],
+                             a["ws"], a["bytes"], None) == status
+    assert L.fluxbin_last_error_message()
+
+
+def test_w4_binding_refusals():
+    """Shapes, types and devices are checked by the binding, before the library's raw pointers."""
+    import torch
+    h = torch.float16
+    for W, g in ((torch.zeros(4, 8, dtype=torch.bfloat16), 8), (torch.zeros(8, dtype=h), 8),
+                 (torch.zeros(4, 8, dtype=h).t(), 4), (torch.zeros(4, 8, dtype=h), 8)):   # the last: not on a GPU
+        with pytest.raises(fb.FluxbinError):
+            fb.fluxbin_w4_quantize(W, g)
+    with pytest.raises(fb.FluxbinError):
+        fb.fluxbin_w4_pack(torch.zeros(4, 1, dtype=torch.int32), torch.zeros(4, 1, dtype=h), None, 8, 8)
