@@ -80,6 +80,90 @@ fluxbin_status fluxbin_w4_gemm(const fluxbin_w4_layer* layer, int32_t B, const u
                                int64_t ldy, int32_t y_is_fp32, void* d_workspace, size_t workspace_bytes,
                                hipStream_t stream);
 
+/*
+ * Paged key/value cache in 8 bits, with one scale for each page (block of tokens) and head, and the attention that reads
+ * it. The value of a cached element is code * scale, code in -127..127, scale fp32.
+ *
+ *   pages      pages of the pool, 1..2^24 (pages * page_size * kv_heads * head_dim <= 2^40).
+ *   page_size  tokens of a page: 16, 32, 64, 128 or 256.
+ *   kv_heads   1..1024.   head_dim  64, 128 or 256.
+ *   d_base     device buffer of fluxbin_kv8_cache_query bytes, 256-byte aligned. It needs no initialization: a page's
+ *              contents are defined by what is appended to it. The layout is private to the library's version.
+ */
+typedef struct {
+  int64_t pages;
+  int32_t page_size, kv_heads, head_dim;
+  uint32_t format_version;
+  void* d_base;
+  uint64_t bytes;
+} fluxbin_kv8_cache;
+#define FLUXBIN_KV8_FORMAT_VERSION 1u
+fluxbin_status fluxbin_kv8_cache_query(int64_t pages, int32_t page_size, int32_t kv_heads, int32_t head_dim,
+                                       size_t* bytes);
+
+/*
+ * The sequences of a call. All arrays are device memory, read by the kernels (so that a captured call serves changing
+ * lengths). Ranges of memory that a call writes may not overlap those it reads, from first to last element.
+ *   rows         rows (tokens) of the call's packed tensors, 0..2^22.    sequences  1..65535.
+ *   d_offsets    int32 [sequences + 1]: sequence b has rows d_offsets[b] .. d_offsets[b+1] - 1, n_b of them. Rows that
+ *                belong to no sequence are neither read nor written; a sequence whose range is not inside [0, rows) is
+ *                left out. Offsets do not fall from one sequence to the next: where they do, what the rows and pages of
+ *                the call get is not defined (nothing else is affected).
+ *   d_context    int32 [sequences]: tokens of each sequence with the call's own among them (taken into 0..2^30): row i of
+ *                a sequence is at position d_context[b] - n_b + i. What is read at a position that was never stored is not
+ *                defined.
+ *   d_block_table  int32 [sequences][max_blocks], row stride block_table_stride >= max_blocks: the page of positions
+ *                p * page_size .. (p + 1) * page_size - 1 is entry p. A position with no entry (negative, or past the table),
+ *                or whose entry is not a page of the pool, is not stored, reads as zero, and is not attended.
+ * Arrays need their elements' alignment.
+ */
+typedef struct {
+  int64_t rows;
+  int32_t sequences, max_blocks;
+  int64_t block_table_stride;
+  const int32_t* d_offsets;
+  const int32_t* d_context;
+  const int32_t* d_block_table;
+} fluxbin_kv8_batch;
+
+/*
+ * Stores the keys and values of the batch's rows. d_k, d_v: fp16, element (row, head, d) at row * token_stride +
+ * head * head_stride + d (strides in elements, >= 0; head_stride at least head_dim if there are several heads; rows may
+ * be slices of a fused projection's rows). For each page and head that gets tokens, keys and values each:
+ *   s = max(s_old if the page holds earlier tokens (its first new position is not its first position), max|new| * (1/127))
+ *   code = rne(v * (1/s)) of a new value, rne(code * (s_old / s)) of an earlier token's where s > s_old
+ * in fp32, 1/s = 0 where s is 0. NaN is stored as 0, infinities as the largest fp16. Positions behind the new ones in
+ * their page lose what they held. A page belongs to one entry of one sequence's table: what a page holds after a call
+ * that stores to it through two entries is not defined (nothing else is affected).
+ */
+fluxbin_status fluxbin_kv8_append(const fluxbin_kv8_cache* cache, const fluxbin_kv8_batch* batch, const uint16_t* d_k,
+                                  int64_t k_token_stride, int64_t k_head_stride, const uint16_t* d_v,
+                                  int64_t v_token_stride, int64_t v_head_stride, hipStream_t stream);
+
+/* The values of the batch's rows from the cache, fp16 [rows][kv_heads][head_dim] each, rounded to nearest even. */
+fluxbin_status fluxbin_kv8_read(const fluxbin_kv8_cache* cache, const fluxbin_kv8_batch* batch, uint16_t* d_k,
+                                uint16_t* d_v, hipStream_t stream);
+
+/*
+ * Attention of the batch's rows over their sequences' cached tokens:
+ *   out[row, h] = sum_j softmax_j(softmax_scale * q[row, h] . k[j, h / (q_heads / kv_heads)]) v[j, ...]
+ * over positions j < d_context[b]; with causal (1) only those up to the row's own position; with window > 0 only those
+ * after the row's position - window. A row without any position is 0.
+ *   d_q, d_out  fp16, element (row, head, d) at row * token_stride + head * head_stride + d, any element alignment.
+ *   q_heads     a multiple of kv_heads, up to 1024.
+ * Scores, softmax sums and results are held in fp32; products are of fp16 operands (codes are exact in fp16, the scales
+ * stay apart), the result is rounded once.
+ * Workspace: partial results of sequences that are split over workgroups; nothing needs clearing; of the size queried
+ * with the largest rows and sequences it serves all smaller calls. Calls that share it must not overlap in time.
+ */
+fluxbin_status fluxbin_kv8_workspace_query(const fluxbin_kv8_cache* cache, int64_t rows, int32_t sequences,
+                                           int32_t q_heads, size_t* bytes);
+fluxbin_status fluxbin_kv8_attention(const fluxbin_kv8_cache* cache, const fluxbin_kv8_batch* batch, int32_t q_heads,
+                                     const uint16_t* d_q, int64_t q_token_stride, int64_t q_head_stride, uint16_t* d_out,
+                                     int64_t out_token_stride, int64_t out_head_stride, float softmax_scale,
+                                     int32_t causal, int32_t window, void* d_workspace, size_t workspace_bytes,
+                                     hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

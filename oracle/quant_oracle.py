@@ -1,4 +1,5 @@
-"""Plain NumPy definitions of the operators declared in include/fluxbin_quant.h: 4-bit linears. What a kernel computes in
+"""Plain NumPy definitions of the operators declared in include/fluxbin_quant.h: 4-bit linears, and the
+paged 8-bit key/value cache with its attention. What a kernel computes in
 32 bits and stores (scales, codes) is computed here with the same 32-bit operations, products and sums in 64 bits."""
 from __future__ import annotations
 
@@ -60,3 +61,117 @@ def w4_bound(W, x, half):
     if half:
         bound = bound * (1 + 2.0 ** -11) + np.abs(x @ W.T) * 2.0 ** -11 + 2.0 ** -25
     return bound
+
+
+# ---------------------------------------------------------------------------------------------- 8-bit cache
+
+class Kv8:
+    """A paged cache: codes int32 [2, pages, P, H, D] and scales fp32 [2, pages, H], keys first."""
+
+    def __init__(self, pages, P, H, D):
+        self.P, self.pages = P, pages
+        self.codes = np.zeros((2, pages, P, H, D), np.int32)
+        self.scales = np.zeros((2, pages, H), F32)
+
+    def page(self, table, b, pos):
+        p = pos // self.P
+        if pos < 0 or p >= table.shape[1]:
+            return -1
+        page = int(table[b, p])
+        return page if 0 <= page < self.pages else -1
+
+    def append(self, k, v, offsets, context, table):
+        """k, v fp16 [T, H, D]."""
+        T = k.shape[0]
+        for b in range(len(context)):
+            o0, o1 = int(offsets[b]), int(offsets[b + 1])
+            if not (0 <= o0 <= o1 <= T):
+                continue
+            i = o0
+            while i < o1:
+                pos = int(context[b]) - (o1 - i)
+                n = 1 if pos < 0 else min(o1 - i, self.P - pos % self.P)
+                page = self.page(table, b, pos)
+                if page >= 0:
+                    for side, x in ((0, k), (1, v)):
+                        self._store(side, page, pos % self.P, x[i:i + n])
+                i += n
+
+    def _store(self, side, page, first, x):
+        x = np.clip(np.nan_to_num(x.astype(F32), nan=0.0, posinf=65504.0, neginf=-65504.0), F32(-65504), F32(65504))
+        old = self.scales[side, page] if first > 0 else np.zeros_like(self.scales[side, page])
+        s = np.maximum(old, np.abs(x).max((0, 2)) * (F32(1) / F32(127)))
+        inv = np.where(s > 0, F32(1) / np.where(s > 0, s, F32(1)), F32(0)).astype(F32)
+        ratio = np.where(s > old, old / np.where(s > 0, s, F32(1)), F32(1)).astype(F32)
+        c = self.codes[side, page]
+        c[:first] = np.rint(c[:first].astype(F32) * ratio[None, :, None]).astype(np.int32)
+        c[first:first + x.shape[0]] = np.clip(np.rint(x * inv[None, :, None]), -127, 127).astype(np.int32)
+        self.scales[side, page] = s
+
+    def values(self, side, b, count, table):
+        """fp64 [count, H, D] of positions 0 .. count - 1, and which of them have a page."""
+        out = np.zeros((count,) + self.codes.shape[3:])
+        ok = np.zeros(count, bool)
+        for p0 in range(0, count, self.P):
+            page, n = self.page(table, b, p0), min(self.P, count - p0)
+            if page >= 0:
+                out[p0:p0 + n] = self.codes[side, page, :n] * self.scales[side, page].astype(np.float64)[None, :, None]
+                ok[p0:p0 + n] = True
+        return out, ok
+
+    def read(self, offsets, context, table, T):
+        """(k, v) fp16 [T, H, D] and the rows that are written."""
+        out = np.zeros((2, T) + self.codes.shape[3:], np.float16)
+        written = np.zeros(T, bool)
+        for b in range(len(context)):
+            o0, o1 = int(offsets[b]), int(offsets[b + 1])
+            if not (0 <= o0 <= o1 <= T):
+                continue
+            written[o0:o1] = True
+            c = max(0, int(context[b]))
+            for side in (0, 1):
+                x, _ = self.values(side, b, c, table)
+                for i in range(o0, o1):
+                    pos = c - (o1 - i)
+                    if pos >= 0:
+                        out[side, i] = x[pos].astype(F32).astype(np.float16)
+        return out[0], out[1], written
+
+    def attention(self, q, offsets, context, table, scale, causal=True, window=0):
+        """out fp64 [T, Hq, D] and, for bounds, sum_j p_j |v_j| and the largest score's magnitude per row and head."""
+        T, Hq, D = q.shape
+        H = self.codes.shape[3]
+        out, mag, big = np.zeros((T, Hq, D)), np.zeros((T, Hq, D)), np.zeros((T, Hq))
+        written = np.zeros(T, bool)
+        for b in range(len(context)):
+            o0, o1 = int(offsets[b]), int(offsets[b + 1])
+            if not (0 <= o0 <= o1 <= T):
+                continue
+            written[o0:o1] = True
+            c = max(0, int(context[b]))
+            n = min(c, table.shape[1] * self.P)
+            k, ok = self.values(0, b, n, table)
+            v, _ = self.values(1, b, n, table)
+            for i in range(o0, o1):
+                pos = c - (o1 - i)
+                j = np.arange(n)
+                seen = ok & (j <= pos if causal else True) & (j > pos - window if window > 0 else True)
+                if not seen.any():
+                    continue
+                for h in range(Hq):
+                    kk, vv = k[seen, h // (Hq // H)], v[seen, h // (Hq // H)]
+                    a = kk @ q[i, h].astype(np.float64) * scale
+                    p = np.exp(a - a.max())
+                    p /= p.sum()
+                    out[i, h], mag[i, h] = p @ vv, p @ np.abs(vv)
+                    big[i, h] = (np.abs(kk) @ np.abs(q[i, h].astype(np.float64))).max() * abs(scale)
+        return out, mag, big, written
+
+
+def attention_bound(out, mag, big, keys):
+    """How far fp32 attention may be from `out`. A score is a sum of D <= 256 exact products: off by at most 300 * 2^-23 of
+    its terms' magnitudes (`big`), and after conversion to base 2 with the logarithm of a scale (up to 2^6) by 8 * 2^-23 of
+    big + 64 more; so every weight by that factor, and 2^-20 for exponentials, reciprocals and its 22 bits; sums over keys
+    by (keys / 4 + 64) * 2^-23. Numerator and denominator both: twice. The result is rounded to fp16."""
+    eps = 2 * ((300 * big + 8 * (big + 64)) * 2.0 ** -23 + 2.0 ** -20 + (keys / 4 + 64) * 2.0 ** -23)
+    return eps[..., None] * mag * (1 + 2.0 ** -11) + np.abs(out) * 2.0 ** -11 + 2.0 ** -25

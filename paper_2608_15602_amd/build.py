@@ -29,7 +29,8 @@ SAN_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=und
 SOURCES = ["fluxbin_host.cpp", "fluxbin_pack.hip", "fluxbin_gemv.hip", "fluxbin_gemm_batch.hip",
            "fluxbin_gemm_mfma.hip", "fluxbin_rc.hip", "fluxbin_noalloc.hip",
            "fluxbin_gemv_rows.hip", "fluxbin_gemm_mfma_rows.hip", "fluxbin_gemm_mx.hip",
-           "fluxbin_gemm_prefill.hip", "fluxbin_quant_host.cpp", "fluxbin_w4.hip"]
+           "fluxbin_gemm_prefill.hip", "fluxbin_quant_host.cpp", "fluxbin_w4.hip",
+           "fluxbin_kv8.hip", "fluxbin_kv8_attention.hip"]
 HOST_SOURCES = ("fluxbin_host.cpp", "fluxbin_quant_host.cpp")   # what --host-sanitizers instruments
 ARCH = "gfx950"
 

@@ -1,4 +1,5 @@
-// Internal declarations of the operators next to the binary linears: 4-bit linears (fluxbin_w4_*).
+// Internal declarations of the operators next to the binary linears: 4-bit linears
+// (fluxbin_w4_*) and the paged 8-bit key/value cache (fluxbin_kv8_*).
 #pragma once
 
 #include "fluxbin_internal.h"
@@ -57,5 +58,60 @@ fluxbin_status launch_w4_pack(const fluxbin_w4_shape& s, const uint32_t* d_codes
 fluxbin_status launch_w4_quantize(const void* d_W, int w_is_fp32, int64_t ldw, const fluxbin_w4_shape& s,
                                   uint32_t* d_codes, uint16_t* d_scales, uint8_t* d_zeros, uint16_t* d_values,
                                   int64_t ldv, hipStream_t stream);
+
+// ---- paged 8-bit key/value cache ----
+// Sections: key codes, value codes (each pages x kv_heads x page_size x head_dim bytes), key scales, value scales.
+struct Kv8Derived {
+  uint64_t off_v, off_ks, off_vs, total;
+};
+
+inline Kv8Derived kv8_derive(int64_t pages, int32_t page_size, int32_t kv_heads, int32_t head_dim) {
+  Kv8Derived d{};
+  const uint64_t heads = uint64_t(pages) * uint64_t(kv_heads);
+  const uint64_t codes = heads * uint64_t(page_size) * uint64_t(head_dim);   // a multiple of 1024
+  d.off_v = codes;
+  d.off_ks = 2 * codes;
+  d.off_vs = d.off_ks + round_up256(heads * 4);
+  d.total = d.off_vs + round_up256(heads * 4);
+  return d;
+}
+
+struct Kv8Args {
+  uint8_t* k;
+  uint8_t* v;
+  float* ks;
+  float* vs;
+  const int32_t* offsets;
+  const int32_t* context;
+  const int32_t* table;
+  int64_t table_stride;
+  int32_t pages, pshift, Hkv, T, B, max_blocks;   // page_size = 1 << pshift
+};
+
+struct Kv8AppendArgs {
+  Kv8Args c;
+  const uint16_t* src[2];      // keys, values
+  int64_t ts[2], hs[2];        // token and head strides
+};
+
+struct Kv8ReadArgs {
+  Kv8Args c;
+  uint16_t* dst[2];
+};
+
+struct Kv8AttnArgs {
+  Kv8Args c;
+  const uint16_t* q;
+  uint16_t* out;
+  float* part;
+  int64_t qts, qhs, ots, ohs;
+  int32_t G, causal, window, wgs;   // query heads per cached head; workgroups that share the work
+  float scale2;                     // softmax_scale * log2(e)
+};
+
+uint64_t kv8_workspace(int32_t D, int cus);
+fluxbin_status launch_kv8_append(const Kv8AppendArgs& a, int D, hipStream_t stream);
+fluxbin_status launch_kv8_read(const Kv8ReadArgs& a, int D, hipStream_t stream);
+fluxbin_status launch_kv8_attention(Kv8AttnArgs a, int D, int cus, hipStream_t stream);
 
 }  // namespace fluxbin

@@ -32,6 +32,8 @@ EXPORTS = (
 # Entry points declared in include/fluxbin_quant.h.
 QUANT_EXPORTS = (
     "fluxbin_w4_quantize", "fluxbin_w4_pack_query", "fluxbin_w4_pack", "fluxbin_w4_workspace_query", "fluxbin_w4_gemm",
+    "fluxbin_kv8_cache_query", "fluxbin_kv8_append", "fluxbin_kv8_read", "fluxbin_kv8_workspace_query",
+    "fluxbin_kv8_attention",
 )
 NOALLOC_SCRATCH_BYTES = 8 << 20
 
@@ -73,6 +75,18 @@ class W4Shape(ctypes.Structure):
 class W4Layer(ctypes.Structure):
     _fields_ = [("shape", W4Shape), ("d_base", ctypes.c_void_p), ("bytes", ctypes.c_uint64),
                 ("format_version", ctypes.c_uint32), ("reserved1", ctypes.c_uint32)]
+
+
+class Kv8CacheDesc(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("format_version", ctypes.c_uint32), ("d_base", ctypes.c_void_p),
+                ("bytes", ctypes.c_uint64)]
+
+
+class Kv8Batch(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("sequences", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
+                ("block_table_stride", ctypes.c_int64), ("d_offsets", ctypes.c_void_p), ("d_context", ctypes.c_void_p),
+                ("d_block_table", ctypes.c_void_p)]
 
 
 class Tuning(ctypes.Structure):
@@ -129,6 +143,13 @@ def lib() -> ctypes.CDLL:
         L.fluxbin_w4_pack.argtypes = [ctypes.POINTER(W4Shape), vp, vp, vp, vp, sz, ctypes.POINTER(W4Layer), vp]
         L.fluxbin_w4_workspace_query.argtypes = [ctypes.POINTER(W4Layer), i32, ctypes.POINTER(sz)]
         L.fluxbin_w4_gemm.argtypes = [ctypes.POINTER(W4Layer), i32, vp, i64, vp, i64, i32, vp, sz, vp]
+        L.fluxbin_kv8_cache_query.argtypes = [i64, i32, i32, i32, ctypes.POINTER(sz)]
+        cache_p, batch_p = ctypes.POINTER(Kv8CacheDesc), ctypes.POINTER(Kv8Batch)
+        L.fluxbin_kv8_append.argtypes = [cache_p, batch_p, vp, i64, i64, vp, i64, i64, vp]
+        L.fluxbin_kv8_read.argtypes = [cache_p, batch_p, vp, vp, vp]
+        L.fluxbin_kv8_workspace_query.argtypes = [cache_p, i64, i32, i32, ctypes.POINTER(sz)]
+        L.fluxbin_kv8_attention.argtypes = [cache_p, batch_p, i32, vp, i64, i64, vp, i64, i64, ctypes.c_float, i32, i32, vp,
+                                            sz, vp]
         for name in EXPORTS + QUANT_EXPORTS:
             if name not in ("fluxbin_status_string", "fluxbin_last_error_message"):
                 getattr(L, name).restype = ctypes.c_int
@@ -472,6 +493,119 @@ def fluxbin_w4_gemm(layer: PackedW4, x, y=None, out_fp32: bool = False, workspac
                                  0 if B == 1 else y.stride(0), 1 if out_fp32 else 0, workspace.data_ptr(),
                                  workspace.numel() * workspace.element_size(), _stream(stream)))
     return y
+
+
+# ---- paged key/value cache in 8 bits ----
+
+class Kv8Cache:
+    """A paged 8-bit key/value cache: its device buffer (torch uint8 tensor, nothing to clear) and C descriptor."""
+
+    def __init__(self, buf, desc: Kv8CacheDesc):
+        self.buf = buf
+        self.desc = desc
+        self.kv_heads, self.head_dim, self.device, self.ref = desc.kv_heads, desc.head_dim, buf.device, ctypes.byref(desc)
+
+
+def fluxbin_kv8_cache_query(pages: int, page_size: int, kv_heads: int, head_dim: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().fluxbin_kv8_cache_query(int(pages), int(page_size), int(kv_heads), int(head_dim), ctypes.byref(n)))
+    return n.value
+
+
+def make_kv8_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, device=None) -> Kv8Cache:
+    import torch
+    n = fluxbin_kv8_cache_query(pages, page_size, kv_heads, head_dim)
+    buf = torch.empty(n, dtype=torch.uint8, device=device or "cuda")
+    return Kv8Cache(buf, Kv8CacheDesc(int(pages), int(page_size), int(kv_heads), int(head_dim), 1, buf.data_ptr(), n))
+
+
+def _kv8_batch(cache: Kv8Cache, rows: int, offsets, context, block_table) -> Kv8Batch:
+    import torch
+    dev, B = cache.device, context.shape[0]
+    if dev.index != torch.cuda.current_device():
+        raise _invalid(f"the cache is on {dev}, which is not the current CUDA (HIP) device")
+    if offsets.dtype != torch.int32 or context.dtype != torch.int32 or block_table.dtype != torch.int32 or \
+            offsets.device != dev or context.device != dev or block_table.device != dev:
+        raise _invalid(f"offsets, context and block_table must be int32 on {dev}")
+    if context.dim() != 1 or offsets.dim() != 1 or offsets.shape[0] != B + 1 or block_table.dim() != 2 or \
+            block_table.shape[0] != B or not (context.is_contiguous() and offsets.is_contiguous()) or \
+            (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+        raise _invalid("offsets must be [B + 1], context [B] (contiguous), block_table [B, blocks] with unit inner stride")
+    blocks = block_table.shape[1]
+    return Kv8Batch(rows, B, blocks, blocks if B == 1 else block_table.stride(0), offsets.data_ptr(), context.data_ptr(),
+                    block_table.data_ptr())
+
+
+def _kv8_rows(cache: Kv8Cache, name: str, t, heads: int):
+    import torch
+    if t.dim() != 3 or t.dtype != torch.float16 or t.device != cache.device or t.shape[1] != heads or \
+            t.shape[2] != cache.head_dim or t.stride(2) != 1:
+        raise _invalid(f"{name} must be fp16 [rows, {heads}, {cache.head_dim}] on {cache.device} with unit inner stride, got "
+                       f"{t.dtype} {tuple(t.shape)}")
+
+
+def fluxbin_kv8_append(cache: Kv8Cache, k, v, offsets, context, block_table, stream=None) -> None:
+    """Store keys and values fp16 [rows, kv_heads, head_dim] (rows and heads at any stride). Sequence b has rows
+    offsets[b] .. offsets[b+1] - 1, its newest context[b] - n_b .. context[b] - 1; its position p is in page
+    block_table[b, p // page_size]. offsets, context and block_table: int32 on the device."""
+    _kv8_rows(cache, "k", k, cache.kv_heads)
+    _kv8_rows(cache, "v", v, cache.kv_heads)
+    if k.shape[0] != v.shape[0]:
+        raise _invalid(f"k has {k.shape[0]} rows, v {v.shape[0]}")
+    b = _kv8_batch(cache, k.shape[0], offsets, context, block_table)
+    _check(lib().fluxbin_kv8_append(cache.ref, ctypes.byref(b), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
+                                    v.stride(0), v.stride(1), _stream(stream)))
+
+
+def fluxbin_kv8_read(cache: Kv8Cache, offsets, context, block_table, rows: int, stream=None):
+    """The cached values (k, v), fp16 [rows, kv_heads, head_dim], of the sequences' newest tokens (as fluxbin_kv8_append
+    counts them). Rows of no sequence are not written."""
+    import torch
+    b = _kv8_batch(cache, int(rows), offsets, context, block_table)
+    k = torch.empty((int(rows), cache.kv_heads, cache.head_dim), dtype=torch.float16, device=cache.device)
+    v = torch.empty_like(k)
+    _check(lib().fluxbin_kv8_read(cache.ref, ctypes.byref(b), k.data_ptr(), v.data_ptr(), _stream(stream)))
+    return k, v
+
+
+def fluxbin_kv8_workspace_query(cache: Kv8Cache, rows: int, sequences: int, q_heads: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().fluxbin_kv8_workspace_query(cache.ref, int(rows), int(sequences), int(q_heads), ctypes.byref(n)))
+    return n.value
+
+
+def make_kv8_workspace(cache: Kv8Cache, rows: int, sequences: int, q_heads: int):
+    """A workspace (torch uint8 tensor, nothing to clear) for attention calls of up to that many rows and sequences."""
+    import torch
+    n = fluxbin_kv8_workspace_query(cache, rows, sequences, q_heads)
+    return torch.empty(max(256, n), dtype=torch.uint8, device=cache.device)
+
+
+def fluxbin_kv8_attention(cache: Kv8Cache, q, offsets, context, block_table, out=None, scale: Optional[float] = None,
+                          causal: bool = True, window: int = 0, workspace=None, stream=None):
+    """Attention of q fp16 [rows, q_heads, head_dim] (rows and heads at any stride) over the cached tokens of the rows'
+    sequences, given as to fluxbin_kv8_append. scale: 1 / sqrt(head_dim) by default. causal: a row attends positions up to
+    its own; window > 0: only those after its own - window. Returns out, fp16 like q; rows of no sequence are not written."""
+    import torch
+    heads = q.shape[1] if q.dim() == 3 else 0
+    _kv8_rows(cache, "q", q, heads)
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.float16, device=q.device)
+    else:
+        _kv8_rows(cache, "out", out, heads)
+        if out.shape[0] != q.shape[0]:
+            raise _invalid(f"q has {q.shape[0]} rows, out {out.shape[0]}")
+    b = _kv8_batch(cache, q.shape[0], offsets, context, block_table)
+    if workspace is None:
+        workspace = make_kv8_workspace(cache, q.shape[0], b.sequences, heads)
+    elif workspace.device != cache.device:
+        raise _invalid(f"workspace is on {workspace.device}, not on {cache.device}")
+    _check(lib().fluxbin_kv8_attention(cache.ref, ctypes.byref(b), heads, q.data_ptr(), q.stride(0), q.stride(1),
+                                       out.data_ptr(), out.stride(0), out.stride(1),
+                                       cache.head_dim ** -0.5 if scale is None else scale, 1 if causal else 0, int(window),
+                                       workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                       _stream(stream)))
+    return out
 
 
 def fluxbin_get_tuning() -> Dict[str, int]:

@@ -132,3 +132,100 @@ def test_w4_binding_refusals():
             fb.fluxbin_w4_quantize(W, g)
     with pytest.raises(fb.FluxbinError):
         fb.fluxbin_w4_pack(torch.zeros(4, 1, dtype=torch.int32), torch.zeros(4, 1, dtype=h), None, 8, 8)
+
+
+# ---------------------------------------------------------------------------------------------- 8-bit cache
+
+@pytest.mark.parametrize("pages,P,H,D", [(1, 16, 1, 64), (1000, 64, 8, 128), (77, 256, 3, 256)])
+def test_kv8_cache_query(L, pages, P, H, D):
+    assert fb.fluxbin_kv8_cache_query(pages, P, H, D) == 2 * pages * P * H * D + 2 * _up(pages * H * 4)
+
+
+@pytest.mark.parametrize("args,status", [
+    ((0, 64, 8, 128), INV), ((-1, 64, 8, 128), INV), (((1 << 24) + 1, 16, 1, 64), INV), ((9, 0, 8, 128), INV),
+    ((9, 48, 8, 128), UNS), ((9, 512, 8, 128), UNS), ((9, 8, 8, 128), UNS), ((9, 64, 0, 128), INV), ((9, 64, 1025, 128), INV),
+    ((9, 64, 8, 0), INV), ((9, 64, 8, 96), UNS), ((9, 64, 8, 512), UNS), ((1 << 24, 256, 1024, 256), UNS)])
+def test_kv8_cache_refused(L, args, status):
+    n = ctypes.c_size_t(7)
+    assert L.fluxbin_kv8_cache_query(*args, ctypes.byref(n)) == status
+    assert L.fluxbin_last_error_message() and n.value == 7
+
+
+def _cache(**kw):
+    d = fb.Kv8CacheDesc(100, 64, 8, 128, 1, 1 << 30, 1 << 26)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+def _batch(**kw):
+    b = fb.Kv8Batch(10, 2, 5, 5, A[0], A[0] + 4096, A[0] + 8192)
+    for k, v in kw.items():
+        setattr(b, k, v)
+    return b
+
+
+BAD_CALLS = [
+    (dict(cache=dict(format_version=0)), INV), (dict(cache=dict(d_base=None)), INV), (dict(cache=dict(d_base=(1 << 30) + 16)), INV),
+    (dict(cache=dict(bytes=1000)), SMALL), (dict(cache=dict(page_size=24)), UNS), (dict(batch=dict(rows=-1)), INV),
+    (dict(batch=dict(rows=(1 << 22) + 1)), INV), (dict(batch=dict(sequences=0)), INV), (dict(batch=dict(sequences=65536)), INV),
+    (dict(batch=dict(max_blocks=0)), INV), (dict(batch=dict(max_blocks=1 << 24, block_table_stride=1 << 24),
+                                             cache=dict(page_size=128)), UNS),
+    (dict(batch=dict(block_table_stride=4)), INV), (dict(batch=dict(d_offsets=None)), INV), (dict(batch=dict(d_context=None)), INV),
+    (dict(batch=dict(d_block_table=None)), INV), (dict(batch=dict(d_block_table=A[0] + 8194)), INV),
+    (dict(batch=dict(d_context=(1 << 30) + 64)), INV)]
+
+
+def _append(L, cache={}, batch={}, **kw):
+    a = dict(k=A[1], kt=1024, kh=128, v=A[2], vt=1024, vh=128)
+    a.update(kw)
+    return L.fluxbin_kv8_append(ctypes.byref(_cache(**cache)), ctypes.byref(_batch(**batch)), a["k"], a["kt"], a["kh"], a["v"],
+                                a["vt"], a["vh"], None)
+
+
+@pytest.mark.parametrize("kw,status", BAD_CALLS + [
+    (dict(k=None), INV), (dict(v=None), INV), (dict(k=A[1] + 1), INV), (dict(kt=-1), INV), (dict(vh=127), INV),
+    (dict(vh=-128), INV), (dict(k=(1 << 30) - 128), INV), (dict(kt=(1 << 36) + 1), INV)])
+def test_kv8_append_refused(L, kw, status):
+    assert _append(L, **kw) == status
+    assert L.fluxbin_last_error_message()
+
+
+def _read(L, cache={}, batch={}, k=A[1], v=A[2]):
+    return L.fluxbin_kv8_read(ctypes.byref(_cache(**cache)), ctypes.byref(_batch(**batch)), k, v, None)
+
+
+@pytest.mark.parametrize("kw,status", BAD_CALLS[:-1] + [
+    (dict(k=None), INV), (dict(v=None), INV), (dict(k=A[1] + 2), INV), (dict(v=A[1]), INV), (dict(k=1 << 30), INV),
+    (dict(v=A[0] - 64), INV)])
+def test_kv8_read_refused(L, kw, status):
+    assert _read(L, **kw) == status
+
+
+def _attention(L, cache={}, batch={}, **kw):
+    a = dict(heads=64, q=A[1], qt=8192, qh=128, out=A[2], ot=8192, oh=128, scale=0.1, causal=1, window=0, ws=A[3], bytes=1 << 40)
+    a.update(kw)
+    return L.fluxbin_kv8_attention(ctypes.byref(_cache(**cache)), ctypes.byref(_batch(**batch)), a["heads"], a["q"], a["qt"],
+                                   a["qh"], a["out"], a["ot"], a["oh"], a["scale"], a["causal"], a["window"], a["ws"],
+                                   a["bytes"], None)
+
+
+@pytest.mark.parametrize("kw,status", BAD_CALLS[:-1] + [
+    (dict(heads=0), INV), (dict(heads=63), INV), (dict(heads=1032), INV), (dict(scale=float("nan")), INV),
+    (dict(scale=float("inf")), INV), (dict(causal=2), INV), (dict(window=-1), INV), (dict(q=None), INV), (dict(out=None), INV),
+    (dict(out=A[2] + 1), INV), (dict(qh=100), INV), (dict(ot=0), INV), (dict(ot=8191), INV)])
+def test_kv8_attention_refused(L, kw, status):
+    assert _attention(L, **kw) == status
+    assert L.fluxbin_last_error_message()
+
+
+def test_kv8_null_structs(L):
+    assert L.fluxbin_kv8_append(None, ctypes.byref(_batch()), A[1], 1024, 128, A[2], 1024, 128, None) == INV
+    assert L.fluxbin_kv8_append(ctypes.byref(_cache()), None, A[1], 1024, 128, A[2], 1024, 128, None) == INV
+    assert L.fluxbin_kv8_cache_query(9, 64, 8, 128, None) == INV
+
+
+def test_kv8_no_rows(L):
+    """A call without rows is valid and launches nothing."""
+    assert _append(L, batch=dict(rows=0), k=None, v=None) == 0
+    assert _read(L, batch=dict(rows=0), k=None, v=None) == 0
