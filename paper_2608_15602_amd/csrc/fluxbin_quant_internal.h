@@ -44,6 +44,8 @@ struct W4Args {
 };
 
 struct W4Plan {
+  bool many;    // the kernel for many batch rows
+  int nw;       // wavefronts of a workgroup
   int bt;       // 16-row batch tiles of a workgroup
   int rt;       // row tiles of a workgroup
   int parts;    // workgroups per row tile, each with a part of the columns

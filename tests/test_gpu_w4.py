@@ -71,6 +71,18 @@ def test_quantize(fb, M, N, g, asym, fp32):
     assert np.array_equal(values.cpu().numpy(), dense.astype(np.float16))
 
 
+def test_quantize_scale_rounds_twice(fb):
+    """The scale is the fp32 product rounded to fp16: over many groups some differ from the exact product rounded once."""
+    import torch
+    log("case quantize many scales")
+    W = weights(4000, 1600, seed=21).astype(np.float32)
+    for asym in (False, True):
+        codes, scales, zeros, _ = fb.fluxbin_w4_quantize(torch.from_numpy(W).cuda(), 32, asymmetric=asym)
+        q, s, z = qo.w4_quantize(W, 32, asym)
+        assert np.array_equal(scales.cpu().numpy().view(np.uint16), s.view(np.uint16))
+        assert np.array_equal(codes.cpu().numpy().view(np.uint32), qo.w4_words(q))
+
+
 def test_quantize_not_finite(fb):
     """NaN counts as 0, infinities and fp32 values past fp16's range as its largest number."""
     import torch
