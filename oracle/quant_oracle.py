@@ -138,10 +138,11 @@ class Kv8:
         return out[0], out[1], written
 
     def attention(self, q, offsets, context, table, scale, causal=True, window=0):
-        """out fp64 [T, Hq, D] and, for bounds, sum_j p_j |v_j| and the largest score's magnitude per row and head."""
+        """out fp64 [T, Hq, D] and, for bounds, sum_j p_j |v_j|, and per row and head the largest score's magnitude and the
+        largest p_j times 127 scales of its page's values."""
         T, Hq, D = q.shape
         H = self.codes.shape[3]
-        out, mag, big = np.zeros((T, Hq, D)), np.zeros((T, Hq, D)), np.zeros((T, Hq))
+        out, mag, big, peak = np.zeros((T, Hq, D)), np.zeros((T, Hq, D)), np.zeros((T, Hq)), np.zeros((T, Hq))
         written = np.zeros(T, bool)
         for b in range(len(context)):
             o0, o1 = int(offsets[b]), int(offsets[b + 1])
@@ -152,26 +153,36 @@ class Kv8:
             n = min(c, table.shape[1] * self.P)
             k, ok = self.values(0, b, n, table)
             v, _ = self.values(1, b, n, table)
-            for i in range(o0, o1):
-                pos = c - (o1 - i)
-                j = np.arange(n)
-                seen = ok & (j <= pos if causal else True) & (j > pos - window if window > 0 else True)
-                if not seen.any():
-                    continue
-                for h in range(Hq):
-                    kk, vv = k[seen, h // (Hq // H)], v[seen, h // (Hq // H)]
-                    a = kk @ q[i, h].astype(np.float64) * scale
-                    p = np.exp(a - a.max())
-                    p /= p.sum()
-                    out[i, h], mag[i, h] = p @ vv, p @ np.abs(vv)
-                    big[i, h] = (np.abs(kk) @ np.abs(q[i, h].astype(np.float64))).max() * abs(scale)
-        return out, mag, big, written
+            scale_at = np.stack([self.scales[1, max(0, self.page(table, b, i))] for i in range(n)] or [np.zeros(H)])
+            pos = c - np.arange(o1 - o0, 0, -1)[:, None]
+            j = np.arange(n)[None]
+            seen = np.broadcast_to(ok[None], (o1 - o0, n)).copy()
+            if causal:
+                seen &= j <= pos
+            if window > 0:
+                seen &= j > pos - window
+            some = seen.any(1)
+            for h in range(Hq):
+                kk, vv, qq = k[:, h // (Hq // H)], v[:, h // (Hq // H)], q[o0:o1, h].astype(np.float64)
+                s = np.where(seen, qq @ kk.T * scale, -np.inf)
+                e = np.exp(s - np.where(some, s.max(1, initial=-np.inf), 0.0)[:, None])
+                e /= np.where(some, e.sum(1), 1.0)[:, None]
+                out[o0:o1, h], mag[o0:o1, h] = e @ vv, e @ np.abs(vv)
+                big[o0:o1, h] = np.where(seen, np.abs(qq) @ np.abs(kk).T, 0.0).max(1, initial=0.0) * abs(scale)
+                peak[o0:o1, h] = (e * 127 * scale_at[:n, h // (Hq // H)]).max(1, initial=0.0)
+        return out, mag, big, peak, written
 
 
-def attention_bound(out, mag, big, keys):
+def attention_bound(out, mag, big, peak, keys, chunk=False):
     """How far fp32 attention may be from `out`. A score is a sum of D <= 256 exact products: off by at most 300 * 2^-23 of
     its terms' magnitudes (`big`), and after conversion to base 2 with the logarithm of a scale (up to 2^6) by 8 * 2^-23 of
     big + 64 more; so every weight by that factor, and 2^-20 for exponentials, reciprocals and its 22 bits; sums over keys
-    by (keys / 4 + 64) * 2^-23. Numerator and denominator both: twice. The result is rounded to fp16."""
+    by (keys / 4 + 64) * 2^-23. Numerator and denominator both: twice. Prompt chunks round the numerator's weights to fp16
+    (half a step: 2^-11). Weights are fed as fp16 numbers of which the largest (with its page's value scale in it) is at
+    least 2^8, and those are multiples of 2^-24: each may be off by 2^-25, 2^-33 of the largest, times a code of up to 127,
+    which is 2^-33 of `peak` for each key. The result is rounded to fp16."""
     eps = 2 * ((300 * big + 8 * (big + 64)) * 2.0 ** -23 + 2.0 ** -20 + (keys / 4 + 64) * 2.0 ** -23)
-    return eps[..., None] * mag * (1 + 2.0 ** -11) + np.abs(out) * 2.0 ** -11 + 2.0 ** -25
+    if chunk:
+        eps = eps + 2.0 ** -11
+    off = eps[..., None] * mag + (keys * 2.0 ** -33 * peak)[..., None]
+    return off * (1 + 2.0 ** -11) + np.abs(out) * 2.0 ** -11 + 2.0 ** -25

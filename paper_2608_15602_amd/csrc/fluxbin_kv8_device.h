@@ -28,16 +28,19 @@ __device__ __forceinline__ int64_t kv_page_offset(const Kv8Args& a, int page, in
   return ((int64_t(page) * a.Hkv + head) << a.pshift) * D;
 }
 
-// The sequence of row t, or -1.
+// The sequence of row t (the same for all lanes of a wavefront), or -1: the last whose offset is not above t, 64 candidates
+// at a time.
 __device__ __forceinline__ int kv_sequence(const Kv8Args& a, int t, int& start, int& end) {
-  int lo = 0, hi = a.B;   // offsets[lo] <= t < offsets[hi] where the offsets do not fall
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (a.offsets[mid] <= t)
-      lo = mid;
-    else
-      hi = mid;
+  const int lane = int(threadIdx.x) & 63;
+  int lo = 0, n = a.B;   // it is one of lo .. lo + n - 1, where the offsets do not fall
+  while (n > 1) {
+    const int step = (n + 63) >> 6, at = lo + lane * step;
+    const uint64_t below = __ballot(lane * step < n && a.offsets[lane * step < n ? at : lo] <= t);
+    const int l = below ? 63 - __clzll((long long)below) : 0;
+    lo += l * step;
+    n = n - l * step < step ? n - l * step : step;
   }
+  lo = __builtin_amdgcn_readfirstlane(lo);
   start = a.offsets[lo];
   end = a.offsets[lo + 1];
   return start >= 0 && end <= a.T && start <= t && t < end ? lo : -1;

@@ -374,6 +374,8 @@ fluxbin_status fluxbin_kv8_attention(const fluxbin_kv8_cache* cache, const fluxb
   const int32_t H = cache->kv_heads, D = cache->head_dim;
   if (q_heads < 1 || q_heads > 1024 || q_heads % H != 0)
     return fail(FLUXBIN_ERR_INVALID_ARG, "q_heads = %d must be a multiple of kv_heads, up to 1024", q_heads);
+  if (batch->rows * (q_heads / H) > (int64_t(1) << 30))   // rows times heads of a group are 32-bit numbers
+    return fail(FLUXBIN_ERR_UNSUPPORTED, "rows * (q_heads / kv_heads) exceeds 2^30");
   if (!(softmax_scale > -1e30f && softmax_scale < 1e30f))
     return fail(FLUXBIN_ERR_INVALID_ARG, "softmax_scale must be a finite number");
   if (causal != 0 && causal != 1) return fail(FLUXBIN_ERR_INVALID_ARG, "causal must be 0 or 1");

@@ -388,6 +388,23 @@ def _on_device(device, **tensors) -> None:
             raise _invalid(f"{name} is on {t.device}, not on {device}")
 
 
+class _Handles:
+    """What the calls of a layer or cache need again and again: looked up once, a small call's time is that of its Python."""
+
+    def __init__(self):
+        import torch
+        self.half, self.single, self.int32 = torch.float16, torch.float32, torch.int32
+        self.empty = torch.empty
+        self.current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+        self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self.lib = lib()
+
+    def stream(self, stream, index: int):
+        if stream is None and self.raw_stream is not None:
+            return self.raw_stream(index)
+        return _stream(stream)
+
+
 def _dense(name: str, t, dtype, shape) -> None:
     if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
         raise _invalid(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} "
@@ -424,6 +441,8 @@ class PackedW4:
         self.buf = buf
         self.layer = layer
         self.M, self.N, self.device, self.ref = layer.shape.M, layer.shape.N, buf.device, ctypes.byref(layer)
+        self.index = buf.device.index
+        self.use = _Handles()
 
     @property
     def shape(self) -> W4Shape:
@@ -470,28 +489,31 @@ def make_w4_workspace(layer: PackedW4, B: int = 1):
 
 def fluxbin_w4_gemm(layer: PackedW4, x, y=None, out_fp32: bool = False, workspace=None, stream=None):
     """y = What x: x fp16 [N] or [B, N] with unit inner stride, y [M] or [B, M]."""
-    import torch
-    M, N, dev = layer.M, layer.N, layer.device
-    dtype = torch.float32 if out_fp32 else torch.float16
+    M, N, index, use = layer.M, layer.N, layer.index, layer.use
+    dtype = use.single if out_fp32 else use.half
     one = x.dim() == 1
-    B = 1 if one else x.shape[0]
-    if y is None:
-        y = torch.empty(M if one else (B, M), dtype=dtype, device=x.device)
-    if x.dtype != torch.float16 or x.device != dev or tuple(x.shape) != ((N,) if one else (B, N)) or \
+    B = 1 if one else x.size(0)
+    if x.dtype is not use.half or x.get_device() != index or x.dim() > 2 or x.size(-1) != N or \
             (N > 1 and x.stride(-1) != 1):
-        raise _invalid(f"x must be fp16 [{N}] or [B, {N}] on {dev} with unit inner stride, got {x.dtype} {tuple(x.shape)}")
-    if y.dtype != dtype or y.device != dev or tuple(y.shape) != ((M,) if one else (B, M)) or (M > 1 and y.stride(-1) != 1):
-        raise _invalid(f"y must be {dtype} {[M] if one else [B, M]} on {dev} with unit inner stride, got {y.dtype} "
-                       f"{tuple(y.shape)}")
-    if dev.index != torch.cuda.current_device():
-        raise _invalid(f"operands are on {dev}, which is not the current CUDA (HIP) device")
+        raise _invalid(f"x must be fp16 [{N}] or [B, {N}] on {layer.device} with unit inner stride, got {x.dtype} "
+                       f"{tuple(x.shape)} on {x.device}")
+    if y is None:
+        y = use.empty(M if one else (B, M), dtype=dtype, device=layer.device)
+    elif y.dtype is not dtype or y.get_device() != index or y.dim() != x.dim() or y.size(-1) != M or \
+            not (one or y.size(0) == B) or (M > 1 and y.stride(-1) != 1):
+        raise _invalid(f"y must be {dtype} {[M] if one else [B, M]} on {layer.device} with unit inner stride, got {y.dtype} "
+                       f"{tuple(y.shape)} on {y.device}")
+    if use.current_device() != index:
+        raise _invalid(f"operands are on {layer.device}, which is not the current CUDA (HIP) device")
     if workspace is None:
         workspace = make_w4_workspace(layer, B)
-    elif workspace.device != dev:
-        raise _invalid(f"workspace is on {workspace.device}, not on {dev}")
-    _check(lib().fluxbin_w4_gemm(layer.ref, B, x.data_ptr(), 0 if B == 1 else x.stride(0), y.data_ptr(),
-                                 0 if B == 1 else y.stride(0), 1 if out_fp32 else 0, workspace.data_ptr(),
-                                 workspace.numel() * workspace.element_size(), _stream(stream)))
+    elif workspace.get_device() != index:
+        raise _invalid(f"workspace is on {workspace.device}, not on {layer.device}")
+    status = use.lib.fluxbin_w4_gemm(layer.ref, B, x.data_ptr(), 0 if B == 1 else x.stride(0), y.data_ptr(),
+                                     0 if B == 1 else y.stride(0), 1 if out_fp32 else 0, workspace.data_ptr(),
+                                     workspace.nbytes, use.stream(stream, index))
+    if status:
+        _check(status)
     return y
 
 
@@ -504,6 +526,8 @@ class Kv8Cache:
         self.buf = buf
         self.desc = desc
         self.kv_heads, self.head_dim, self.device, self.ref = desc.kv_heads, desc.head_dim, buf.device, ctypes.byref(desc)
+        self.index = buf.device.index
+        self.use = _Handles()
 
 
 def fluxbin_kv8_cache_query(pages: int, page_size: int, kv_heads: int, head_dim: int) -> int:
@@ -520,51 +544,54 @@ def make_kv8_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, dev
 
 
 def _kv8_batch(cache: Kv8Cache, rows: int, offsets, context, block_table) -> Kv8Batch:
-    import torch
-    dev, B = cache.device, context.shape[0]
-    if dev.index != torch.cuda.current_device():
-        raise _invalid(f"the cache is on {dev}, which is not the current CUDA (HIP) device")
-    if offsets.dtype != torch.int32 or context.dtype != torch.int32 or block_table.dtype != torch.int32 or \
-            offsets.device != dev or context.device != dev or block_table.device != dev:
-        raise _invalid(f"offsets, context and block_table must be int32 on {dev}")
-    if context.dim() != 1 or offsets.dim() != 1 or offsets.shape[0] != B + 1 or block_table.dim() != 2 or \
-            block_table.shape[0] != B or not (context.is_contiguous() and offsets.is_contiguous()) or \
-            (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+    index, int32 = cache.index, cache.use.int32
+    if cache.use.current_device() != index:
+        raise _invalid(f"the cache is on {cache.device}, which is not the current CUDA (HIP) device")
+    if offsets.dtype is not int32 or context.dtype is not int32 or block_table.dtype is not int32 or \
+            offsets.get_device() != index or context.get_device() != index or block_table.get_device() != index:
+        raise _invalid(f"offsets, context and block_table must be int32 on {cache.device}")
+    if context.dim() != 1 or offsets.dim() != 1 or block_table.dim() != 2:
+        raise _invalid("offsets must be [B + 1], context [B], block_table [B, blocks]")
+    B, blocks = block_table.shape
+    if context.size(0) != B or offsets.size(0) != B + 1 or not (context.is_contiguous() and offsets.is_contiguous()) or \
+            (blocks > 1 and block_table.stride(1) != 1):
         raise _invalid("offsets must be [B + 1], context [B] (contiguous), block_table [B, blocks] with unit inner stride")
-    blocks = block_table.shape[1]
     return Kv8Batch(rows, B, blocks, blocks if B == 1 else block_table.stride(0), offsets.data_ptr(), context.data_ptr(),
                     block_table.data_ptr())
 
 
-def _kv8_rows(cache: Kv8Cache, name: str, t, heads: int):
-    import torch
-    if t.dim() != 3 or t.dtype != torch.float16 or t.device != cache.device or t.shape[1] != heads or \
-            t.shape[2] != cache.head_dim or t.stride(2) != 1:
+def _kv8_rows(cache: Kv8Cache, name: str, t, heads: int) -> int:
+    if t.dim() != 3 or t.dtype is not cache.use.half or t.get_device() != cache.index or t.size(1) != heads or \
+            t.size(2) != cache.head_dim or t.stride(2) != 1:
         raise _invalid(f"{name} must be fp16 [rows, {heads}, {cache.head_dim}] on {cache.device} with unit inner stride, got "
-                       f"{t.dtype} {tuple(t.shape)}")
+                       f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.size(0)
 
 
 def fluxbin_kv8_append(cache: Kv8Cache, k, v, offsets, context, block_table, stream=None) -> None:
     """Store keys and values fp16 [rows, kv_heads, head_dim] (rows and heads at any stride). Sequence b has rows
     offsets[b] .. offsets[b+1] - 1, its newest context[b] - n_b .. context[b] - 1; its position p is in page
     block_table[b, p // page_size]. offsets, context and block_table: int32 on the device."""
-    _kv8_rows(cache, "k", k, cache.kv_heads)
-    _kv8_rows(cache, "v", v, cache.kv_heads)
-    if k.shape[0] != v.shape[0]:
-        raise _invalid(f"k has {k.shape[0]} rows, v {v.shape[0]}")
-    b = _kv8_batch(cache, k.shape[0], offsets, context, block_table)
-    _check(lib().fluxbin_kv8_append(cache.ref, ctypes.byref(b), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
-                                    v.stride(0), v.stride(1), _stream(stream)))
+    rows = _kv8_rows(cache, "k", k, cache.kv_heads)
+    if rows != _kv8_rows(cache, "v", v, cache.kv_heads):
+        raise _invalid(f"k has {rows} rows, v {v.shape[0]}")
+    b = _kv8_batch(cache, rows, offsets, context, block_table)
+    status = cache.use.lib.fluxbin_kv8_append(cache.ref, ctypes.byref(b), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
+                                              v.stride(0), v.stride(1), cache.use.stream(stream, cache.index))
+    if status:
+        _check(status)
 
 
 def fluxbin_kv8_read(cache: Kv8Cache, offsets, context, block_table, rows: int, stream=None):
     """The cached values (k, v), fp16 [rows, kv_heads, head_dim], of the sequences' newest tokens (as fluxbin_kv8_append
     counts them). Rows of no sequence are not written."""
-    import torch
-    b = _kv8_batch(cache, int(rows), offsets, context, block_table)
-    k = torch.empty((int(rows), cache.kv_heads, cache.head_dim), dtype=torch.float16, device=cache.device)
-    v = torch.empty_like(k)
-    _check(lib().fluxbin_kv8_read(cache.ref, ctypes.byref(b), k.data_ptr(), v.data_ptr(), _stream(stream)))
+    use, rows = cache.use, int(rows)
+    b = _kv8_batch(cache, rows, offsets, context, block_table)
+    shape = (rows, cache.kv_heads, cache.head_dim)
+    k, v = (use.empty(shape, dtype=use.half, device=cache.device) for _ in "kv")
+    status = use.lib.fluxbin_kv8_read(cache.ref, ctypes.byref(b), k.data_ptr(), v.data_ptr(), use.stream(stream, cache.index))
+    if status:
+        _check(status)
     return k, v
 
 
@@ -586,25 +613,24 @@ def fluxbin_kv8_attention(cache: Kv8Cache, q, offsets, context, block_table, out
     """Attention of q fp16 [rows, q_heads, head_dim] (rows and heads at any stride) over the cached tokens of the rows'
     sequences, given as to fluxbin_kv8_append. scale: 1 / sqrt(head_dim) by default. causal: a row attends positions up to
     its own; window > 0: only those after its own - window. Returns out, fp16 like q; rows of no sequence are not written."""
-    import torch
-    heads = q.shape[1] if q.dim() == 3 else 0
-    _kv8_rows(cache, "q", q, heads)
+    use, heads = cache.use, q.size(1) if q.dim() == 3 else 0
+    rows = _kv8_rows(cache, "q", q, heads)
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float16, device=q.device)
-    else:
-        _kv8_rows(cache, "out", out, heads)
-        if out.shape[0] != q.shape[0]:
-            raise _invalid(f"q has {q.shape[0]} rows, out {out.shape[0]}")
-    b = _kv8_batch(cache, q.shape[0], offsets, context, block_table)
+        out = use.empty(q.shape, dtype=use.half, device=cache.device)
+    elif rows != _kv8_rows(cache, "out", out, heads):
+        raise _invalid(f"q has {rows} rows, out {out.shape[0]}")
+    b = _kv8_batch(cache, rows, offsets, context, block_table)
     if workspace is None:
-        workspace = make_kv8_workspace(cache, q.shape[0], b.sequences, heads)
-    elif workspace.device != cache.device:
+        workspace = make_kv8_workspace(cache, rows, b.sequences, heads)
+    elif workspace.get_device() != cache.index:
         raise _invalid(f"workspace is on {workspace.device}, not on {cache.device}")
-    _check(lib().fluxbin_kv8_attention(cache.ref, ctypes.byref(b), heads, q.data_ptr(), q.stride(0), q.stride(1),
-                                       out.data_ptr(), out.stride(0), out.stride(1),
-                                       cache.head_dim ** -0.5 if scale is None else scale, 1 if causal else 0, int(window),
-                                       workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                       _stream(stream)))
+    status = use.lib.fluxbin_kv8_attention(cache.ref, ctypes.byref(b), heads, q.data_ptr(), q.stride(0), q.stride(1),
+                                           out.data_ptr(), out.stride(0), out.stride(1),
+                                           cache.head_dim ** -0.5 if scale is None else scale, 1 if causal else 0,
+                                           int(window), workspace.data_ptr(), workspace.nbytes,
+                                           use.stream(stream, cache.index))
+    if status:
+        _check(status)
     return out
 
 

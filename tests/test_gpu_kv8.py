@@ -72,7 +72,7 @@ class Setup:
         pk, pv, _ = self.plain.read(offsets, self.length, self.table, T)
         assert np.array_equal(k.cpu().numpy(), pk) and np.array_equal(v.cpu().numpy(), pv)
 
-    def attend(self, new, G, causal=True, window=0, scale=None, q=None, ws=None):
+    def attend(self, new, G, causal=True, window=0, scale=None, q=None, ws=None, chunk=False):
         """Queries of the newest new[b] tokens, as slices of longer rows; rows of nobody stay as they were."""
         offsets = np.concatenate([[0], np.cumsum(new)])
         T, Hq = int(offsets[-1]), self.H * G
@@ -88,10 +88,10 @@ class Setup:
         got = back.cpu().double().numpy()
         assert (got[T] == 7).all() and (got[:, 0] == 7).all()
         got = got[:T, 1:].reshape(T, Hq, self.D)
-        ref, mag, big, written = self.plain.attention(q, offsets, self.length, self.table,
+        ref, mag, big, peak, written = self.plain.attention(q, offsets, self.length, self.table,
                                                       self.D ** -0.5 if scale is None else scale, causal, window)
         assert written.all()
-        bound = qo.attention_bound(ref, mag, big, max(1, int(self.length.max())))
+        bound = qo.attention_bound(ref, mag, big, peak, max(1, int(self.length.max())), chunk)
         far = np.abs(got - ref) / bound
         log(f"  worst {far.max():.3f} of the bound")
         assert (far <= 1).all()
@@ -174,9 +174,9 @@ def test_bad_pages_and_lengths(fb):
         assert np.array_equal(kt.cpu().numpy()[written], pk[written]) and np.array_equal(vt.cpu().numpy()[written], pv[written])
         out = s.torch.full((20, 4, 64), 7.0, dtype=s.torch.float16, device="cuda")
         fb.fluxbin_kv8_attention(s.cache, s.dev(q), *a, out=out)
-        ref, mag, big, _ = s.plain.attention(q, offs, near, s.table, 0.125)
+        ref, mag, big, peak, _ = s.plain.attention(q, offs, near, s.table, 0.125)
         got = out.cpu().double().numpy()
-        assert (np.abs(got - ref)[written] <= qo.attention_bound(ref, mag, big, 128)[written]).all()
+        assert (np.abs(got - ref)[written] <= qo.attention_bound(ref, mag, big, peak, 128)[written]).all()
         assert (got[~written] == 7).all()
     s.table = good
     s.length[:] = [36, 60, 0, 0, 0]
@@ -265,6 +265,36 @@ def test_prompt_chunks(fb, new, ctx):
         s.append(new)
         s.attend(new, G)
         s.attend(new, G, window=100)
+
+
+@pytest.mark.parametrize("H,G,D,P,new,ctx", [
+    (8, 8, 64, 16, [301, 211], [301, 500]), (8, 8, 128, 64, [300, 1, 230], [333, 90, 700]), (8, 8, 256, 32, [270], [400]),
+    (32, 1, 128, 128, [1030], [1030]), (7, 5, 64, 256, [500, 471], [500, 2000])])
+def test_many_rows(fb, H, G, D, P, new, ctx):
+    """Enough rows for the prompt chunks' own kernel, ragged, masked and not."""
+    log(f"case many rows H={H} G={G} D={D} P={P} new={new} ctx={ctx}")
+    assert sum(new) * G // (64 if D == 256 else 128) * H >= 256   # where that kernel takes over on 256 CUs
+    s = Setup(fb, len(new), H, D, P, max(ctx), seed=20)
+    s.append([c - n for c, n in zip(ctx, new)])
+    s.append(new)
+    s.attend(new, G, chunk=True)
+    s.attend(new, G, window=77, chunk=True)
+    s.attend(new, G, causal=False, chunk=True)
+    s.length[0] -= 40                           # rows before position 0 (or fewer tokens)
+    s.table[-1, 1] = -1                         # a page that is missing
+    got = s.attend(new, G, chunk=True)
+    if ctx[0] == new[0]:
+        assert (got[:40] == 0).all()
+
+
+def test_many_rows_scales_far_apart(fb):
+    log("case many rows, scales far apart")
+    s = Setup(fb, 1, 16, 64, 16, 512, seed=22)
+    for i in range(32):
+        s.append([16], 1.0, lambda k, v, i=i: v.__imul__(np.float16([1e-7, 1e3, 1.0, 0.0, 1e-3][i % 5])))
+    q = (s.rng.standard_normal((512, 64, 64)) * 3).astype(np.float16)
+    s.attend([512], 4, q=q, chunk=True)
+    s.attend([512], 4, causal=False, q=q, scale=0.5, chunk=True)
 
 
 def test_scales_far_apart(fb):

@@ -211,7 +211,7 @@ def _attention(L, cache={}, batch={}, **kw):
 
 
 @pytest.mark.parametrize("kw,status", BAD_CALLS[:-1] + [
-    (dict(heads=0), INV), (dict(heads=63), INV), (dict(heads=1032), INV), (dict(scale=float("nan")), INV),
+    (dict(heads=0), INV), (dict(heads=63), INV), (dict(heads=1024, batch=dict(rows=1 << 22), cache=dict(kv_heads=1)), UNS), (dict(heads=1032), INV), (dict(scale=float("nan")), INV),
     (dict(scale=float("inf")), INV), (dict(causal=2), INV), (dict(window=-1), INV), (dict(q=None), INV), (dict(out=None), INV),
     (dict(out=A[2] + 1), INV), (dict(qh=100), INV), (dict(ot=0), INV), (dict(ot=8191), INV)])
 def test_kv8_attention_refused(L, kw, status):
