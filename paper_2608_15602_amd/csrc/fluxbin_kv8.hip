@@ -8,12 +8,13 @@ namespace {
 // Eight new elements as they are stored: NaN as 0, an infinity as the largest fp16. Returns the bits of the largest magnitude
 // (the order of fp16 magnitudes is that of their bits).
 __device__ __forceinline__ uint32_t kv_clean8(uint16_t (&h)[8]) {
-  uint32_t most = 0;
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  uint32_t w[4];
+  __builtin_memcpy(w, h, 16);
+  u16x2 pair = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t m = h[i] & 0x7FFFu;
-    most = m > most ? m : most;
-  }
+  for (int i = 0; i < 4; ++i) pair = __builtin_elementwise_max(pair, __builtin_bit_cast(u16x2, w[i] & 0x7FFF7FFFu));
+  uint32_t most = pair.x > pair.y ? pair.x : pair.y;
   if (most < 0x7C00u) return most;   // nearly always: all finite
   most = 0;
 #pragma unroll
@@ -150,10 +151,10 @@ __device__ void kv_store_page(const Kv8AppendArgs& a, int page, int head, int ro
   }
 }
 
-// Workgroup (window of `span` rows, head, side): the rows of its window that are the first of their sequence or of their
-// page start a page's new tokens.
+// Workgroup (window of `span` rows, `heads` heads, side): the rows of its window that are the first of their sequence or of
+// their page start a page's new tokens.
 template <int D>
-__global__ void __launch_bounds__(256) k_kv8_append(Kv8AppendArgs a, int span) {
+__global__ void __launch_bounds__(256) k_kv8_append(Kv8AppendArgs a, int span, int heads) {
   __shared__ float red[5];
   __shared__ __attribute__((aligned(16))) uint16_t slab[kSlab][D];
   const Kv8Args& c = a.c;
@@ -170,11 +171,14 @@ __global__ void __launch_bounds__(256) k_kv8_append(Kv8AppendArgs a, int span) {
     const int page = kv_page(c, b, pos);
     if (page < 0) continue;
     const int first = pos & (P - 1), left = end - t, count = left < P - first ? left : P - first;
-    __syncthreads();   // red and slab of the page before
-    if (blockIdx.z == 0)
-      kv_store_page<D, 0>(a, page, int(blockIdx.y), t, first, count, red, slab);
-    else
-      kv_store_page<D, 1>(a, page, int(blockIdx.y), t, first, count, red, slab);
+    const int h1 = int(blockIdx.y) * heads + heads < c.Hkv ? int(blockIdx.y) * heads + heads : c.Hkv;
+    for (int h = int(blockIdx.y) * heads; h < h1; ++h) {
+      __syncthreads();   // red and slab of the page or head before
+      if (blockIdx.z == 0)
+        kv_store_page<D, 0>(a, page, h, t, first, count, red, slab);
+      else
+        kv_store_page<D, 1>(a, page, h, t, first, count, red, slab);
+    }
   }
 }
 
@@ -242,9 +246,9 @@ static int rows_per_window(const Kv8Args& c, int most) {
 
 template <int D>
 void append_launch(const Kv8AppendArgs& a, hipStream_t stream) {
-  const int span = rows_per_window(a.c, 1 << a.c.pshift);
-  const dim3 grid(unsigned(ceil_div(a.c.T, span)), unsigned(a.c.Hkv), 2);
-  hipLaunchKernelGGL(k_kv8_append<D>, grid, dim3(256), 0, stream, a, span);
+  const int span = rows_per_window(a.c, 1 << a.c.pshift), heads = span > 1 ? 2 : 1;
+  const dim3 grid(unsigned(ceil_div(a.c.T, span)), unsigned(ceil_div(a.c.Hkv, heads)), 2);
+  hipLaunchKernelGGL(k_kv8_append<D>, grid, dim3(256), 0, stream, a, span, heads);
 }
 
 template <int D>

@@ -458,7 +458,7 @@ __device__ __forceinline__ kv_h4 codes4(uint32_t a) {
 }
 
 template <int D, int CT, int NW>
-__global__ void __launch_bounds__(64 * NW, 2) k_kv8_chunk(Kv8AttnArgs a) {
+__global__ void __launch_bounds__(64 * NW, CT == 4 ? 1 : 2) k_kv8_chunk(Kv8AttnArgs a) {
   constexpr int kCols = 16 * CT * NW, kF = D / 32, kE = D / 16, kU = D / 64;
   constexpr int kParts = NW / 4;   // wavefronts that share a block of 16 tokens: one does keys and values, or one each
   __shared__ __attribute__((aligned(16))) kv_h8 lk[2][4 * kF * 64], lv[2][2 * kE * 64];   // [block][f][lane], [pair][e][lane]
@@ -519,12 +519,15 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_chunk(Kv8AttnArgs a) {
   const int any_lo = a.window > 0 && first_pos + r_lo + 1 > a.window ? first_pos + r_lo + 1 - a.window : 0;
 
   kv_f4 o[CT][kE];
-  float mx[CT], sum[CT];
+  // p = 2^(s - base); a base is kShift below a column's first scores' maximum, and moves when scores come to be more than
+  // kShift + kSlack above it. limit: what is above it, or anything finite before the first.
+  float base[CT], limit[CT], sum[CT];
 #pragma unroll
   for (int t = 0; t < CT; ++t) {
 #pragma unroll
     for (int e = 0; e < kE; ++e) o[t][e] = kv_f4{0.f, 0.f, 0.f, 0.f};
-    mx[t] = -__builtin_inff();
+    base[t] = 0.f;
+    limit[t] = -__builtin_inff();
     sum[t] = 0.f;
   }
 
@@ -607,23 +610,25 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_chunk(Kv8AttnArgs a) {
       }
       kv_f4 sc[CT][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int f = 0; f < kF; ++f)
 #pragma unroll
-        for (int c = 0; c < CT; ++c) sc[c][j] = kv_f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int f = 0; f < kF; ++f) {
+        for (int j = 0; j < 4; ++j) {
           const kv_h8 k = lk[buf][(j * kF + f) * 64 + lane];
 #pragma unroll
-          for (int c = 0; c < CT; ++c) sc[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[c][f], sc[c][j], 0, 0, 0);
+          for (int c = 0; c < CT; ++c) {
+            if (f == 0) sc[c][j] = kv_f4{0.f, 0.f, 0.f, 0.f};
+            sc[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[c][f], sc[c][j], 0, 0, 0);
+          }
         }
-      }
       kv_h8 ph[CT][2];
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j) {
+          const float add = lj[j] - base[c];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sc[c][j][i] = __builtin_fmaf(sc[c][j][i], kj[j], lj[j]);
+          for (int i = 0; i < 4; ++i) sc[c][j][i] = __builtin_fmaf(sc[c][j][i], kj[j], add);
+        }
         if (tok < all_lo || tok + kTile > all_hi) {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
@@ -640,19 +645,24 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_chunk(Kv8AttnArgs a) {
           for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[c][j][i]);
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        if (__any(top > mx[c] + kSlack)) {
-          const float now = fmaxf(mx[c], top), r = now == mx[c] ? 1.f : __builtin_amdgcn_exp2f(mx[c] - now);
+        if (__any(top > limit[c])) {   // scores that are too large for the columns' bases, or their first
+          // columns with none keep theirs; `by` is finite where there is a score
+          const float by = top > limit[c] ? top - kShift : 0.f, r = limit[c] < 0.f ? 0.f : __builtin_amdgcn_exp2f(-by);
           sum[c] *= r;
 #pragma unroll
           for (int e = 0; e < kE; ++e) o[c][e] *= r;
-          mx[c] = now;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[c][j][i] -= by;
+          base[c] += by;
+          limit[c] = top > limit[c] ? kShift + kSlack : limit[c];
         }
-        const float base = mx[c] == -__builtin_inff() ? 0.f : mx[c] - kShift;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float p = __builtin_amdgcn_exp2f(sc[c][j][i] - base);
+            const float p = __builtin_amdgcn_exp2f(sc[c][j][i]);
             // p before it is rounded: a weight on values of a tiny scale may be lost in p, but not in the sum
             sum[c] = __builtin_fmaf(p, rj[j], sum[c]);
             ph[c][j >> 1][4 * (j & 1) + i] = _Float16(p);
