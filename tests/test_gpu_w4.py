@@ -131,6 +131,49 @@ def test_gemm(fb, M, N, g, asym):
             assert (y == 7).all()
 
 
+# layers tall enough for two row tiles a workgroup, with and without chunks after the last whole step; long enough for every
+# number of wavefronts and for the many-row kernel's parts
+LARGE = [(8200, 600, 64, True), (4100, 2050, 128, False), (8200, 2112, 32, True), (8210, 4224, 128, True), (2000, 9000, 256, True),
+         (16400, 520, 64, False)]
+
+
+@pytest.mark.parametrize("M,N,g,asym", LARGE)
+def test_gemm_large(fb, M, N, g, asym):
+    import torch
+    codes, scales, zeros = canonical(M, N, g, asym, seed=M + N)
+    layer = pack(fb, codes, scales, zeros, g, asym)
+    W = qo.w4_dense(codes, scales, zeros, g)
+    x = (np.random.default_rng(N).standard_normal((256, N))).astype(np.float16)
+    ref, bound = x.astype(np.float64) @ W.T, qo.w4_bound(W, x.astype(np.float64), False)
+    xt, ws = torch.from_numpy(x).cuda(), fb.make_w4_workspace(layer, 256)
+    for B in (1, 4, 5, 16, 17, 32, 40, 48, 64, 100, 256):
+        log(f"case gemm M={M} N={N} g={g} asym={asym} B={B}")
+        ws.fill_(0xFF)
+        y = fb.fluxbin_w4_gemm(layer, xt[:B], out_fp32=True, workspace=ws).cpu().double().numpy()
+        assert (np.abs(y - ref[:B]) <= bound[:B]).all()
+
+
+def test_workspace_refusals(fb):
+    import torch
+    log("case gemm refusals")
+    codes, scales, zeros = canonical(48, 20000, 128, True, seed=9)
+    layer = pack(fb, codes, scales, zeros, 128, True)
+    x = torch.randn(16, 20000, device="cuda").half()
+    n = fb.fluxbin_w4_workspace_query(layer, 16)
+    assert n > 0
+    for ws in (torch.empty(256, dtype=torch.uint8, device="cuda"), torch.empty(n, dtype=torch.uint8), layer.buf,
+               torch.empty(n + 8, dtype=torch.uint8, device="cuda")[8:]):
+        with pytest.raises(fb.FluxbinError):
+            fb.fluxbin_w4_gemm(layer, x, workspace=ws)
+    for bad in (x.float(), x[:, :-1], x.cpu(), x.t(), x[None], x.repeat(1, 2)[:, ::2]):
+        with pytest.raises(fb.FluxbinError):
+            fb.fluxbin_w4_gemm(layer, bad)
+    for bad in (x[:, :48], torch.empty(16, 48, device="cuda"), torch.empty(15, 48, dtype=torch.float16, device="cuda"),
+                torch.empty(16, 49, dtype=torch.float16, device="cuda")):
+        with pytest.raises(fb.FluxbinError):
+            fb.fluxbin_w4_gemm(layer, x, y=bad)
+
+
 def test_gemv_is_the_first_row(fb):
     """A vector gives what a batch of one gives, with and without given outputs and workspaces, twice the same bits."""
     import torch
