@@ -106,10 +106,17 @@ struct Walk {
     }
     return sum;
   }
-  // The sequence that holds unit u (before the total, not before an earlier call's), and its first unit.
+  // The sequence that holds unit u (before the total, not before an earlier call's), and its first unit. n = 0: there is
+  // none (lengths that change while a call reads them), so that the walk ends whatever it reads.
   __device__ __forceinline__ Seq find(int64_t u, int64_t& first) {
     uint64_t hit;
-    while ((hit = __ballot(upto > u)) == 0) next();
+    while ((hit = __ballot(upto > u)) == 0) {
+      if (base + 64 >= a.c.B) {
+        Seq none = {};
+        return none;
+      }
+      next();
+    }
     const int l = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)hit) - 1);
     Seq s;
     s.start = __builtin_amdgcn_readlane(mine.start, l);
@@ -175,6 +182,7 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_attention
   for (int64_t u = u0; u < u1;) {
     int64_t first;
     const Seq s = walk.find(u, first);
+    if (s.n == 0) break;
     const int64_t rel = u - first;
     const int item = a.whole ? int(rel) : int(quotient(rel, s.nt));   // column tile, head
     const int ta = a.whole ? 0 : int(rel - int64_t(item) * s.nt);
@@ -384,7 +392,7 @@ __global__ void __launch_bounds__(512) k_kv8_join(Kv8AttnArgs a) {
   __shared__ kv_f4 sums[512];
   __shared__ float tops[512], ls[512];
   const Joint it = reinterpret_cast<const Joint*>(a.part + int64_t(a.wgs) * 2 * part_floats<D>())[blockIdx.x];
-  if (it.last == 0) return;
+  if (it.last == 0 || it.last >= a.wgs) return;
   const int tid = int(threadIdx.x), slice = tid / D, c = int(blockIdx.y) * 4 + tid % D / (D / 4), d = tid % (D / 4) * 4;
   const int w0 = int(blockIdx.x);
   const float* parts = a.part + int64_t(w0) * 2 * part_floats<D>();

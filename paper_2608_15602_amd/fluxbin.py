@@ -399,6 +399,15 @@ class _Handles:
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self.lib = lib()
 
+    def new(self, stream, *size, dtype, device):
+        """A tensor whose memory belongs to the stream that the call runs on (the allocator may give memory that other
+        work on the current stream still uses, and give it away again before another stream is done with it)."""
+        if stream is None:
+            return self.empty(size, dtype=dtype, device=device)
+        import torch
+        with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))):
+            return self.empty(size, dtype=dtype, device=device)
+
     def stream(self, stream, index: int):
         if stream is None and self.raw_stream is not None:
             return self.raw_stream(index)
@@ -423,7 +432,8 @@ def fluxbin_w4_quantize(W, g: int, asymmetric: bool = True, values: bool = False
     if g < 1:
         raise _invalid(f"g = {g} must be >= 1")
     G = -(-N // g)
-    new = lambda dtype, *size: torch.empty(size, dtype=dtype, device=W.device)
+    use = _Handles()
+    new = lambda dtype, *size: use.new(stream, *size, dtype=dtype, device=W.device)
     codes, scales = new(torch.int32, M, -(-N // 8)), new(torch.float16, M, G)
     zeros = new(torch.uint8, M, G) if asymmetric else None
     out = new(torch.float16, M, N) if values else None
@@ -468,7 +478,7 @@ def fluxbin_w4_pack(codes, scales, zeros, N: int, g: int, stream=None) -> Packed
         _dense("zeros", zeros, torch.uint8, (M, G))
     shape = W4Shape(M, int(N), int(g), 0 if zeros is None else 1, 0)
     n = fluxbin_w4_pack_query(shape)
-    buf = torch.empty(n, dtype=torch.uint8, device=codes.device)
+    buf = _Handles().new(stream, n, dtype=torch.uint8, device=codes.device)
     out = W4Layer()
     _check(lib().fluxbin_w4_pack(ctypes.byref(shape), codes.data_ptr(), scales.data_ptr(), _ptr(zeros), buf.data_ptr(), n,
                                  ctypes.byref(out), _stream(stream)))
@@ -481,10 +491,10 @@ def fluxbin_w4_workspace_query(layer: PackedW4, B: int = 1) -> int:
     return n.value
 
 
-def make_w4_workspace(layer: PackedW4, B: int = 1):
+def make_w4_workspace(layer: PackedW4, B: int = 1, stream=None):
     """A workspace (torch uint8 tensor, nothing to clear) for calls of up to B rows."""
     import torch
-    return torch.empty(max(256, fluxbin_w4_workspace_query(layer, B)), dtype=torch.uint8, device=layer.device)
+    return layer.use.new(stream, max(256, fluxbin_w4_workspace_query(layer, B)), dtype=torch.uint8, device=layer.device)
 
 
 def fluxbin_w4_gemm(layer: PackedW4, x, y=None, out_fp32: bool = False, workspace=None, stream=None):
@@ -498,7 +508,7 @@ def fluxbin_w4_gemm(layer: PackedW4, x, y=None, out_fp32: bool = False, workspac
         raise _invalid(f"x must be fp16 [{N}] or [B, {N}] on {layer.device} with unit inner stride, got {x.dtype} "
                        f"{tuple(x.shape)} on {x.device}")
     if y is None:
-        y = use.empty(M if one else (B, M), dtype=dtype, device=layer.device)
+        y = use.new(stream, *((M,) if one else (B, M)), dtype=dtype, device=layer.device)
     elif y.dtype is not dtype or y.get_device() != index or y.dim() != x.dim() or y.size(-1) != M or \
             not (one or y.size(0) == B) or (M > 1 and y.stride(-1) != 1):
         raise _invalid(f"y must be {dtype} {[M] if one else [B, M]} on {layer.device} with unit inner stride, got {y.dtype} "
@@ -506,7 +516,7 @@ def fluxbin_w4_gemm(layer: PackedW4, x, y=None, out_fp32: bool = False, workspac
     if use.current_device() != index:
         raise _invalid(f"operands are on {layer.device}, which is not the current CUDA (HIP) device")
     if workspace is None:
-        workspace = make_w4_workspace(layer, B)
+        workspace = make_w4_workspace(layer, B, stream)
     elif workspace.get_device() != index:
         raise _invalid(f"workspace is on {workspace.device}, not on {layer.device}")
     status = use.lib.fluxbin_w4_gemm(layer.ref, B, x.data_ptr(), 0 if B == 1 else x.stride(0), y.data_ptr(),
@@ -587,8 +597,7 @@ def fluxbin_kv8_read(cache: Kv8Cache, offsets, context, block_table, rows: int, 
     counts them). Rows of no sequence are not written."""
     use, rows = cache.use, int(rows)
     b = _kv8_batch(cache, rows, offsets, context, block_table)
-    shape = (rows, cache.kv_heads, cache.head_dim)
-    k, v = (use.empty(shape, dtype=use.half, device=cache.device) for _ in "kv")
+    k, v = (use.new(stream, rows, cache.kv_heads, cache.head_dim, dtype=use.half, device=cache.device) for _ in "kv")
     status = use.lib.fluxbin_kv8_read(cache.ref, ctypes.byref(b), k.data_ptr(), v.data_ptr(), use.stream(stream, cache.index))
     if status:
         _check(status)
@@ -601,11 +610,11 @@ def fluxbin_kv8_workspace_query(cache: Kv8Cache, rows: int, sequences: int, q_he
     return n.value
 
 
-def make_kv8_workspace(cache: Kv8Cache, rows: int, sequences: int, q_heads: int):
+def make_kv8_workspace(cache: Kv8Cache, rows: int, sequences: int, q_heads: int, stream=None):
     """A workspace (torch uint8 tensor, nothing to clear) for attention calls of up to that many rows and sequences."""
     import torch
     n = fluxbin_kv8_workspace_query(cache, rows, sequences, q_heads)
-    return torch.empty(max(256, n), dtype=torch.uint8, device=cache.device)
+    return cache.use.new(stream, max(256, n), dtype=torch.uint8, device=cache.device)
 
 
 def fluxbin_kv8_attention(cache: Kv8Cache, q, offsets, context, block_table, out=None, scale: Optional[float] = None,
@@ -616,18 +625,18 @@ def fluxbin_kv8_attention(cache: Kv8Cache, q, offsets, context, block_table, out
     use, heads = cache.use, q.size(1) if q.dim() == 3 else 0
     rows = _kv8_rows(cache, "q", q, heads)
     if out is None:
-        out = use.empty(q.shape, dtype=use.half, device=cache.device)
+        out = use.new(stream, *q.shape, dtype=use.half, device=cache.device)
     elif rows != _kv8_rows(cache, "out", out, heads):
         raise _invalid(f"q has {rows} rows, out {out.shape[0]}")
     b = _kv8_batch(cache, rows, offsets, context, block_table)
     if workspace is None:
-        workspace = make_kv8_workspace(cache, rows, b.sequences, heads)
+        workspace = make_kv8_workspace(cache, rows, b.sequences, heads, stream)
     elif workspace.get_device() != cache.index:
         raise _invalid(f"workspace is on {workspace.device}, not on {cache.device}")
     status = use.lib.fluxbin_kv8_attention(cache.ref, ctypes.byref(b), heads, q.data_ptr(), q.stride(0), q.stride(1),
                                            out.data_ptr(), out.stride(0), out.stride(1),
                                            cache.head_dim ** -0.5 if scale is None else scale, 1 if causal else 0,
-                                           int(window), workspace.data_ptr(), workspace.nbytes,
+                                           min(int(window), 0x7FFFFFFF), workspace.data_ptr(), workspace.nbytes,
                                            use.stream(stream, cache.index))
     if status:
         _check(status)

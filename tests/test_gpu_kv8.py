@@ -367,6 +367,34 @@ def test_graph_with_growing_lengths(fb):
     assert torch.isfinite(out).all() and n > 0
 
 
+def test_cache_past_32_bits(fb):
+    """Pages whose codes lie past 2^32 bytes, and scales far into their sections."""
+    import torch
+    log("case large cache")
+    H, D, P, pages = 8, 128, 64, 70000
+    assert pages * H * D * P > 2 ** 32
+    s = Setup(fb, 2, H, D, P, 3 * P, seed=23)
+    del s.cache
+    s.cache = fb.make_kv8_cache(pages, P, H, D)
+    low = s.table
+    high = np.array([[pages - 1, 0, pages - 2], [pages // 2, pages - 3, 65536]], np.int32)
+    q = s.rng.standard_normal((2, 16, D)).astype(np.float16)
+    k, v = s.rows(250)
+    offsets, lengths = [0, 150, 250], np.array([150, 100])
+    a = s.ints(offsets), s.ints(lengths), s.ints(high)
+    fb.fluxbin_kv8_append(s.cache, s.dev(k), s.dev(v), *a)
+    s.plain.append(k, v, offsets, lengths, low)
+    kt, vt = fb.fluxbin_kv8_read(s.cache, *a, 250)
+    pk, pv, _ = s.plain.read(offsets, lengths, low, 250)
+    assert np.array_equal(kt.cpu().numpy(), pk) and np.array_equal(vt.cpu().numpy(), pv)
+    out = fb.fluxbin_kv8_attention(s.cache, s.dev(q), s.ints([0, 1, 2]), a[1], a[2]).cpu().double().numpy()
+    ref, mag, big, peak, _ = s.plain.attention(q, [0, 1, 2], lengths, low, D ** -0.5)
+    assert (np.abs(out - ref) <= qo.attention_bound(ref, mag, big, peak, 150)).all()
+    del kt, vt
+    s.cache = None
+    torch.cuda.empty_cache()
+
+
 def test_another_stream(fb):
     import torch
     log("case stream")
@@ -381,3 +409,10 @@ def test_another_stream(fb):
     fb.fluxbin_kv8_attention(s.cache, q, *a, out=out, workspace=ws, stream=side)
     side.synchronize()
     assert torch.equal(out, ref)
+    side.wait_stream(torch.cuda.current_stream())
+    for handle in (side, side.cuda_stream):   # outputs and workspaces of the call's own, on its stream
+        out = fb.fluxbin_kv8_attention(s.cache, q, *a, stream=handle)
+        k, v = fb.fluxbin_kv8_read(s.cache, *a, 2, stream=handle)
+        side.synchronize()
+        assert torch.equal(out, ref)
+        assert all(torch.equal(x, y) for x, y in zip((k, v), fb.fluxbin_kv8_read(s.cache, *a, 2)))
