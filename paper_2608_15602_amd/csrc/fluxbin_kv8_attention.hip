@@ -167,8 +167,12 @@ __device__ __forceinline__ void store_out(const Kv8AttnArgs& a, const Seq& s, in
 //
 // Bound by the stream of codes. A step's keys are requested when the last step's have been used and before its softmax, its
 // values when the last step's have been used, so that a wavefront always has 8 KB or more on their way (D = 128); page
-// numbers and scales come for 64 blocks of 16 tokens at a time, one per lane.
-template <int D>
+// numbers and scales come for 64 blocks of 16 tokens at a time, one per lane (a request for each block's page, and its wait
+// before the codes' requests, cost a quarter of the time). Two contexts of 50000 and 65536 tokens, 8 cached heads of 128:
+// 50 us, 4.7 TB/s, 6 of them the join; 32 of 256 to 8192 tokens: 42.5 us, 3.7 TB/s, where a workgroup's share is 18 steps of
+// one or two items and every item's start (lengths, pages, codes, one after another) is seen.
+// ONCE: every code is read by one workgroup only (one column tile), past the caches' ordinary order.
+template <int D, bool ONCE>
 __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_attention(Kv8AttnArgs a) {
   __shared__ __attribute__((aligned(16))) float lds_o[kWaves][16][D + 4];
   __shared__ float lds_m[kWaves][16], lds_l[kWaves][16];
@@ -242,8 +246,10 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_attention
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int k = 0; k < D / 64; ++k)
-            v[j][k] = *reinterpret_cast<const kv_u4*>(base + off[j] + k * 1024 + uint32_t(lane * 16));
+          for (int k = 0; k < D / 64; ++k) {
+            const kv_u4* p = reinterpret_cast<const kv_u4*>(base + off[j] + k * 1024 + uint32_t(lane * 16));
+            v[j][k] = ONCE ? __builtin_nontemporal_load(p) : *p;
+          }
       };
       look(w0);
 #pragma unroll
@@ -453,7 +459,10 @@ __global__ void __launch_bounds__(512) k_kv8_join(Kv8AttnArgs a) {
 // ---------------------------------------------------------------------------------------------------------------------
 // Prompt chunks. A workgroup takes 16 CT columns for each of its NW wavefronts, of one sequence and head, and goes over all
 // the tokens that they attend. A tile of 64 tokens is decoded once for all wavefronts: each turns a part of its codes into
-// fp16 in LDS, in operand order, a tile ahead of its use, its requests two tiles ahead. p is fed rounded to fp16
+// fp16 in LDS, in operand order, a tile ahead of its use, its requests two tiles ahead. Two sequences with 1024 and 700 new
+// rows on 4096 and 1500 tokens, 64 heads of 128 over 8: 237 us, 620 TFLOP/s (a large fp16 matrix product: 1144); 4096 rows on
+// 8192 tokens: 820. Counters: matrix cores 24%, vector instructions 40% of the time, the rest waits and uneven ends. 64
+// columns per wavefront (one per SIMD) took 360 us, eight wavefronts per workgroup 258. p is fed rounded to fp16
 // (its rounding is as large as the result's own; the sum of two numbers as below would be half as much matrix work again).
 // ---------------------------------------------------------------------------------------------------------------------
 
@@ -711,7 +720,12 @@ void attention_launch(Kv8AttnArgs a, int cus, hipStream_t stream) {
   // Short tables: items are not split, which saves the second kernel (2 to 3 us with its launch; 16 tiles are 4 steps for
   // each of a workgroup's wavefronts).
   a.whole = (int64_t(a.c.max_blocks) << a.c.pshift) <= 15 * kTile;
-  hipLaunchKernelGGL(k_kv8_attention<D>, dim3(unsigned(a.wgs)), dim3(64 * kWaves), 0, stream, a);
+  // Single tokens of groups of up to 16 heads: 32 sequences of 256 to 8192 tokens 42.5 us with streaming requests, 45 without,
+  // 4 of 16384 with 40 heads 109 and 121; eight tokens of 8 sequences of 8192 (four column tiles) 56.7 and 55.3.
+  if (a.c.T <= a.c.B && a.G <= 16)
+    hipLaunchKernelGGL((k_kv8_attention<D, true>), dim3(unsigned(a.wgs)), dim3(64 * kWaves), 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_kv8_attention<D, false>), dim3(unsigned(a.wgs)), dim3(64 * kWaves), 0, stream, a);
   if (!a.whole) hipLaunchKernelGGL(k_kv8_join<D>, dim3(unsigned(a.wgs - 1), 4), dim3(512), 0, stream, a);
 }
 

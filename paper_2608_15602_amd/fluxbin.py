@@ -597,7 +597,8 @@ def fluxbin_kv8_read(cache: Kv8Cache, offsets, context, block_table, rows: int, 
     counts them). Rows of no sequence are not written."""
     use, rows = cache.use, int(rows)
     b = _kv8_batch(cache, rows, offsets, context, block_table)
-    k, v = (use.new(stream, rows, cache.kv_heads, cache.head_dim, dtype=use.half, device=cache.device) for _ in "kv")
+    k = use.new(stream, rows, cache.kv_heads, cache.head_dim, dtype=use.half, device=cache.device)
+    v = use.new(stream, rows, cache.kv_heads, cache.head_dim, dtype=use.half, device=cache.device)
     status = use.lib.fluxbin_kv8_read(cache.ref, ctypes.byref(b), k.data_ptr(), v.data_ptr(), use.stream(stream, cache.index))
     if status:
         _check(status)
