@@ -48,7 +48,7 @@ __device__ __forceinline__ Seq seq_of(const Kv8AttnArgs& a, int b) {
   int begin = 0;
   if (a.window > 0 && s.ctx - s.n + 1 > a.window) begin = s.ctx - s.n + 1 - a.window;
   if (begin > s.end) begin = s.end;
-  s.qt = (s.n * a.G + 15) >> 4;
+  s.qt = s.n * a.G >= a.chunk_from ? 0 : (s.n * a.G + 15) >> 4;   // the others are the prompt chunks' kernel's
   s.t0 = begin / kTile;
   s.nt = (s.end + kTile - 1) / kTile - s.t0;
   if (s.nt < 1) s.nt = 1;   // nothing to attend: one tile, all of it masked
@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(64 * NW, CT == 4 ? 1 : 2) k_kv8_chunk(Kv8AttnA
     int nb = 0;
     if (mine_b < a.c.B) {
       const int o0 = a.c.offsets[mine_b], o1 = a.c.offsets[mine_b + 1];
-      if (o0 >= 0 && o1 <= a.c.T && o1 > o0) nb = ((o1 - o0) * a.G + kCols - 1) / kCols;
+      if (o0 >= 0 && o1 <= a.c.T && o1 > o0 && (o1 - o0) * a.G >= a.chunk_from) nb = ((o1 - o0) * a.G + kCols - 1) / kCols;
     }
     int upto = nb;
 #pragma unroll
@@ -708,14 +708,18 @@ __global__ void __launch_bounds__(64 * NW, CT == 4 ? 1 : 2) k_kv8_chunk(Kv8AttnA
 
 int attention_wgs(int cus) { return 2 * cus; }
 
-// Prompt chunks where they fill the chip: a workgroup of four wavefronts, 32 columns each (16 for D = 256).
+// Prompt chunks where they fill the chip: a workgroup of four wavefronts, 32 columns each (16 for D = 256). Sequences with
+// fewer rows than one workgroup's columns among them go to the other kernel, which splits their tokens: one workgroup would
+// take 1.6 us for every 64 tokens of a long context.
 template <int D>
 void attention_launch(Kv8AttnArgs a, int cus, hipStream_t stream) {
   constexpr int CT = D == 256 ? 1 : 2, cols = 64 * CT;
   const int64_t blocks = int64_t(a.c.T) * a.G / cols;
+  a.chunk_from = INT32_MAX;
   if (blocks * a.c.Hkv >= cus && blocks >= a.c.B) {
+    a.chunk_from = a.c.B > 1 ? cols : 0;
     hipLaunchKernelGGL((k_kv8_chunk<D, CT, 4>), dim3(unsigned(blocks + a.c.B), unsigned(a.c.Hkv)), dim3(256), 0, stream, a);
-    return;
+    if (a.c.B == 1) return;
   }
   // Short tables: items are not split, which saves the second kernel (2 to 3 us with its launch; 16 tiles are 4 steps for
   // each of a workgroup's wavefronts).

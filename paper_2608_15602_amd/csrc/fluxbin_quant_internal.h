@@ -108,6 +108,7 @@ struct Kv8AttnArgs {
   float* part;
   int64_t qts, qhs, ots, ohs;
   int32_t G, causal, window, wgs;   // query heads per cached head; workgroups that share the work
+  int32_t chunk_from;               // columns (rows times G) of a sequence from which the prompt chunks' kernel takes it
   int32_t whole;                    // 1: a sequence's column tile and head is not split over workgroups
   float scale2;                     // softmax_scale * log2(e)
 };

@@ -287,6 +287,18 @@ def test_many_rows(fb, H, G, D, P, new, ctx):
         assert (got[:40] == 0).all()
 
 
+def test_single_tokens_among_many_rows(fb):
+    """Single tokens of long and short contexts, sequences without rows, and prompts in one call."""
+    log("case mixed batch")
+    s = Setup(fb, 7, 8, 128, 64, 5000, seed=24)
+    new, ctx = [1, 600, 0, 3, 1, 16, 2], [5000, 600, 40, 900, 1, 77, 2]
+    s.append([c - n for c, n in zip(ctx, new)])
+    s.append(new)
+    assert sum(new) * 8 // 128 * 8 >= 256
+    s.attend(new, 8, chunk=True)
+    s.attend(new, 8, window=700, chunk=True)
+
+
 def test_many_rows_scales_far_apart(fb):
     log("case many rows, scales far apart")
     s = Setup(fb, 1, 16, 64, 16, 512, seed=22)
