@@ -84,8 +84,7 @@ struct Walk {
     mine = seq_of(a, b < a.c.B ? b : a.c.B - 1);
     if (b >= a.c.B) mine.qt = 0;
     int64_t v = units_of(a, mine);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
+    for (int o = 1; o < 64 && o < a.c.B; o <<= 1) {   // lanes past the last sequence: not whole sums
       const int64_t u = __shfl_up(v, o);
       if (lane >= o) v += u;
     }
@@ -97,7 +96,7 @@ struct Walk {
     load();
   }
   __device__ __forceinline__ int64_t total() {
-    int64_t sum = uniform64(__shfl(upto, 63));
+    int64_t sum = uniform64(__shfl(upto, a.c.B < 64 ? a.c.B - 1 : 63));
     for (int b = 64 + lane; b - lane < a.c.B; b += 64) {
       int64_t v = b < a.c.B ? units_of(a, seq_of(a, b)) : 0;
 #pragma unroll
@@ -212,6 +211,12 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_attention
     const int per = (tb - ta + kWaves - 1) / kWaves, w0 = ta + wave * per;
     const int w1 = w0 + per < tb ? w0 + per : tb;
     if (w0 < w1) {
+      kv_h8 qf[D / 32];
+      {
+        const uint16_t* p = a.q + int64_t(s.start + (has ? ci : 0)) * a.qts + int64_t(head * a.G + (has ? cg : 0)) * a.qhs;
+#pragma unroll
+        for (int f = 0; f < D / 32; ++f) __builtin_memcpy(&qf[f], p + 32 * f + 8 * q4, 16);   // no such column: never stored
+      }
       // blocks of 16 tokens 4 (t0 + w) + lane .. of 16 steps: page, key scale with the softmax's, value scale's logarithm
       // and reciprocal; a block without a page: a logarithm that masks it
       int page;
@@ -257,12 +262,6 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_attention
       load(a.c.k, kw);
       load(a.c.v, vw);
       scales();
-      kv_h8 qf[D / 32];
-      {
-        const uint16_t* p = a.q + int64_t(s.start + (has ? ci : 0)) * a.qts + int64_t(head * a.G + (has ? cg : 0)) * a.qhs;
-#pragma unroll
-        for (int f = 0; f < D / 32; ++f) __builtin_memcpy(&qf[f], p + 32 * f + 8 * q4, 16);   // no such column: never stored
-      }
       for (int w = w0; w < w1; ++w) {
         const int tok = (s.t0 + w) * kTile;
         float kj[4], lj[4], rj[4];
