@@ -693,10 +693,17 @@ W4Plan w4_plan(const fluxbin_w4_shape& s, int B, int cus) {
     // two row tiles share the activations' way through LDS: 28672x8192 at B = 16 36 us, 43 with one; at B = 4 31 and 29
     p.rt = 2;
     p.nw = waves(ceil_div(d.Mt, 2), 8, 8);
-  } else {
-    // 16 wavefronts per CU: 28672x8192 at B = 1 28 us with 2 of them in a workgroup, 33 with 8; 8192x28672 48 and 27
+  } else if (B > 4) {
     p.rt = 1;
-    p.nw = waves(d.Mt, 16, B <= 4 ? 16 : 8);
+    p.nw = waves(d.Mt, 16, 8);
+  } else {
+    // six wavefronts per CU, and more while each has six steps: at B = 1 28672x8192 30.4 us with 4 in a workgroup, 35.4 with 2,
+    // 38 with 16; 8192x28672 28 with 16, 31 with 4; 14336x4096 11.0 with 2, 11.4 with 8; 8192x8192 11.4 with 4, 12.6 with 16
+    p.rt = 1;
+    p.nw = 2;
+    while (p.nw < 16 && p.nw < steps && (d.Mt * p.nw < 6 * cus || steps >= 6 * p.nw)) p.nw *= 2;
+  }
+  if (p.rt == 1) {
     // few rows and many columns: 512x28672 at B = 1 11.5 us, 8.8 with 4 parts; 512x4096 3.9 and 6.0
     const int64_t room = 2 * cus / (d.Mt * ceil_div(B, 32));
     int64_t parts = steps / p.nw < room ? steps / p.nw : room;
