@@ -71,9 +71,10 @@ fluxbin_status fluxbin_w4_pack(const fluxbin_w4_shape* shape, const uint32_t* d_
  * Y[b, :] = W-hat X[b, :] for b < B (1..8192). d_x fp16 with row stride ldx >= N, any alignment of an element; d_y fp16 or
  * fp32 with row stride ldy >= M; strides in elements, for B = 1 not used. (q - z) x is summed in fp32 from exact products
  * and multiplied by the scale once per group of at most 128 columns.
- * Workspace: partial sums where the columns are split over workgroups, or the call's activations in operand order; every
- * call rewrites what it reads, nothing needs clearing, and the workspace queried for B serves every smaller batch and any
- * layer whose query is no larger. It may be NULL where the query says 0. Calls that share it must not overlap in time.
+ * Workspace: partial sums where the columns are split over workgroups; every call writes what it reads, nothing needs
+ * clearing, and the workspace queried for B serves every smaller batch and any layer whose query is no larger. It may be
+ * NULL where the query says 0. Calls that share it must not overlap in time. Memory that a call writes may not overlap
+ * memory that it reads, from first to last element.
  */
 fluxbin_status fluxbin_w4_workspace_query(const fluxbin_w4_layer* layer, int32_t B, size_t* bytes);
 fluxbin_status fluxbin_w4_gemm(const fluxbin_w4_layer* layer, int32_t B, const uint16_t* d_x, int64_t ldx, void* d_y,
@@ -151,8 +152,10 @@ fluxbin_status fluxbin_kv8_read(const fluxbin_kv8_cache* cache, const fluxbin_kv
  * after the row's position - window. A row without any position is 0.
  *   d_q, d_out  fp16, element (row, head, d) at row * token_stride + head * head_stride + d, any element alignment.
  *   q_heads     a multiple of kv_heads, up to 1024.
- * Scores, softmax sums and results are held in fp32; products are of fp16 operands (codes are exact in fp16, the scales
- * stay apart), the result is rounded once.
+ * Scores, softmax sums and results are held in fp32; products are of fp16 operands: codes, which are exact in fp16 (their
+ * scales stay apart), and softmax weights, as the sum of two fp16 numbers or, where a call's rows fill the device as prompt
+ * chunks, as one. A row's result may differ in its last bits between a call that has it among many rows and one that does
+ * not.
  * Workspace: partial results of sequences that are split over workgroups; nothing needs clearing; of the size queried
  * with the largest rows and sequences it serves all smaller calls. Calls that share it must not overlap in time.
  */

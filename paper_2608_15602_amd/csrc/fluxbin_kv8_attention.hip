@@ -168,7 +168,7 @@ __device__ __forceinline__ void store_out(const Kv8AttnArgs& a, const Seq& s, in
 // values when the last step's have been used, so that a wavefront always has 8 KB or more on their way (D = 128); page
 // numbers and scales come for 64 blocks of 16 tokens at a time, one per lane (a request for each block's page, and its wait
 // before the codes' requests, cost a quarter of the time). Two contexts of 50000 and 65536 tokens, 8 cached heads of 128:
-// 50 us, 4.7 TB/s, 6 of them the join; 32 of 256 to 8192 tokens: 42.5 us, 3.7 TB/s, where a workgroup's share is 18 steps of
+// 50 us, 4.7 TB/s, 6 of them the join; 32 of 256 to 8192 tokens: 43 us, 3.6 TB/s, where a workgroup's share is 18 steps of
 // one or two items and every item's start (lengths, pages, codes, one after another) is seen.
 // ONCE: every code is read by one workgroup only (one column tile), past the caches' ordinary order.
 template <int D, bool ONCE>
@@ -459,9 +459,10 @@ __global__ void __launch_bounds__(512) k_kv8_join(Kv8AttnArgs a) {
 // Prompt chunks. A workgroup takes 16 CT columns for each of its NW wavefronts, of one sequence and head, and goes over all
 // the tokens that they attend. A tile of 64 tokens is decoded once for all wavefronts: each turns a part of its codes into
 // fp16 in LDS, in operand order, a tile ahead of its use, its requests two tiles ahead. Two sequences with 1024 and 700 new
-// rows on 4096 and 1500 tokens, 64 heads of 128 over 8: 237 us, 620 TFLOP/s (a large fp16 matrix product: 1144); 4096 rows on
-// 8192 tokens: 820. Counters: matrix cores 24%, vector instructions 40% of the time, the rest waits and uneven ends. 64
-// columns per wavefront (one per SIMD) took 360 us, eight wavefronts per workgroup 258. p is fed rounded to fp16
+// rows on 4096 and 1500 tokens, 64 heads of 128 over 8: 243 us, 600 TFLOP/s, 7 of them the launches for sequences of few
+// rows (a large fp16 matrix product: 1144); 4096 rows on 8192 tokens: 820. Counters: matrix cores 24%, vector instructions
+// 40% of the time, the rest waits and uneven ends. 64 columns per wavefront (one per SIMD) took 360 us with the chunks'
+// launch alone, eight wavefronts per workgroup 258, this form 237. p is fed rounded to fp16
 // (its rounding is as large as the result's own; the sum of two numbers as below would be half as much matrix work again).
 // ---------------------------------------------------------------------------------------------------------------------
 

@@ -187,8 +187,8 @@ __global__ void __launch_bounds__(256) k_w4_pack_scales(const uint16_t* scales, 
 // a wavefront keeps a step (4 RT KB) of requests ahead. Activations go through the wavefront's own LDS: a request takes
 // four whole row pieces of 256 bytes (XR requests a chunk), and lanes pick their operands from there: straight from memory
 // an operand is 64 bytes of each of 16 rows, and such requests took 2.5 times as long and bound the kernel (8192x28672 at
-// B = 16: 65 us with them). 28672x8192 with zero points per group of 128 at B = 1: 33 us among other calls, 28 in a graph
-// of such calls (122 MB, 4.4 TB/s); 8192x28672 at B = 16: 37 us; 4096x4096 at B = 1: 5 us.
+// B = 16: 65 us with them). 28672x8192 with zero points per group of 128 at B = 1: 29 us (122 MB, 4.2 TB/s; the kernel
+// alone 24.5, 5.0 TB/s); 8192x28672 at B = 16: 37 us; 4096x4096 at B = 1: 5 us.
 // ---------------------------------------------------------------------------------------------------------------------
 
 // Eight activations from column c of a row, zero past its end: the requests go out together, past the end for the last
