@@ -153,9 +153,10 @@ fluxbin_status fluxbin_kv8_read(const fluxbin_kv8_cache* cache, const fluxbin_kv
  *   d_q, d_out  fp16, element (row, head, d) at row * token_stride + head * head_stride + d, any element alignment.
  *   q_heads     a multiple of kv_heads, up to 1024.
  * Scores, softmax sums and results are held in fp32; products are of fp16 operands: codes, which are exact in fp16 (their
- * scales stay apart), and softmax weights, as the sum of two fp16 numbers or, where a call's rows fill the device as prompt
- * chunks, as one. A row's result may differ in its last bits between a call that has it among many rows and one that does
- * not.
+ * scales stay apart), and softmax weights times their page's value scale, as the sum of two fp16 numbers: such a product is
+ * off by at most 2^-21 of itself and 2^-33 of the row's largest one (an element in which the tokens of the largest products
+ * have code 0 is as far off as that leaves it). A row's result may differ in its last bits between a call that has it among
+ * many rows and one that does not.
  * Workspace: partial results of sequences that are split over workgroups; nothing needs clearing; of the size queried
  * with the largest rows and sequences it serves all smaller calls. Calls that share it must not overlap in time.
  */

@@ -173,16 +173,37 @@ class Kv8:
         return out, mag, big, peak, written
 
 
-def attention_bound(out, mag, big, peak, keys, chunk=False):
+def attention_bound(out, mag, big, peak, keys, chunk=False, log2_scale=64):
     """How far fp32 attention may be from `out`. A score is a sum of D <= 256 exact products: off by at most 300 * 2^-23 of
-    its terms' magnitudes (`big`), and after conversion to base 2 with the logarithm of a scale (up to 2^6) by 8 * 2^-23 of
-    big + 64 more; so every weight by that factor, and 2^-20 for exponentials, reciprocals and its 22 bits; sums over keys
-    by (keys / 4 + 64) * 2^-23. Numerator and denominator both: twice. Prompt chunks round the numerator's weights to fp16
-    (half a step: 2^-11). Weights are fed as fp16 numbers of which the largest (with its page's value scale in it) is at
-    least 2^8, and those are multiples of 2^-24: each may be off by 2^-25, 2^-33 of the largest, times a code of up to 127,
-    which is 2^-33 of `peak` for each key. The result is rounded to fp16."""
-    eps = 2 * ((300 * big + 8 * (big + 64)) * 2.0 ** -23 + 2.0 ** -20 + (keys / 4 + 64) * 2.0 ** -23)
+    its terms' magnitudes (`big`), and after conversion to base 2 with the logarithm of a scale (up to 2^6, or what the
+    caller knows: `log2_scale`) by 8 * 2^-23 of big + 64 more; so every weight by that factor, and 2^-20 for exponentials,
+    reciprocals and its 21 bits; sums over keys by (keys / 4 + 64) * 2^-23. Numerator and denominator both: twice. Weights
+    are fed as fp16 numbers of which the largest (with its page's value scale in it) is at least 2^8, and those are
+    multiples of 2^-24: each may be off by 2^-25, 2^-33 of the largest, times a code of up to 127, which is 2^-33 of `peak`
+    for each key. The result is rounded to fp16. chunk: room for weights of one fp16 number (half a step: 2^-11), which no
+    form has; attention_apart tells them."""
+    eps = 2 * ((300 * big + 8 * (big + log2_scale)) * 2.0 ** -23 + 2.0 ** -20 + (keys / 4 + 64) * 2.0 ** -23)
     if chunk:
         eps = eps + 2.0 ** -11
     off = eps[..., None] * mag + (keys * 2.0 ** -33 * peak)[..., None]
     return off * (1 + 2.0 ** -11) + np.abs(out) * 2.0 ** -11 + 2.0 ** -25
+
+
+# Norm of the difference to the fp16-rounded reference, relative to the reference's norm, that attention in fp32 with weights
+# of two fp16 numbers may have on ordinary data (attention_apart).
+APART = 2.0 ** -13
+
+
+def attention_apart(got, ref):
+    """How far fp16 results are from the 64-bit reference rounded to fp16, relative to the reference's norm: what is left
+    when the final rounding, which would cover errors of its own size, is taken out.
+
+    An element whose value before that rounding is off by e differs by a step u where a border between two fp16 numbers
+    lies between it and the reference, which over many elements happens to |e| / u of them. The sum of the squares is then
+    about the sum of |e| u, at most |e| |u| <= t 2^-10 of the reference's square where t is the error's norm relative to the
+    reference's. fp32 arithmetic whose roundings are independent has t below 2^-17: scores of magnitude up to 16 are rounded
+    a few times (2^-21 each time), their sums over D <= 256 products add sqrt(D) 2^-24 of the largest, sums over keys less,
+    a weight of two fp16 numbers 2^-21. So the result is below 2^-13.5, and APART is one and a half times that. One fp16
+    number for a weight (t = 2^-12.3) gives 2^-11.2; scores in fp16 (2^-11 of magnitudes above 1) or weights in bf16 more."""
+    ref = np.asarray(ref, np.float64)
+    return float(np.linalg.norm(np.asarray(got, np.float64) - ref.astype(np.float16).astype(np.float64)) / np.linalg.norm(ref))

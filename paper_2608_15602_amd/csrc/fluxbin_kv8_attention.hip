@@ -5,7 +5,9 @@
 // Codes are exact in fp16, so K and V enter as codes and the scales, one per page and head, stay apart: the key's multiplies
 // the score in fp32; the value's is added to the score as its logarithm, p = 2^(s + log2 sv - m), so that O sums p * code
 // and the softmax sum is that of p / sv. With m the running maximum of s + log2 sv no p leaves fp16's range, however the
-// scales of the pages differ. Single tokens feed p as the sum of two fp16 numbers (22 bits).
+// scales of the pages differ. p is fed as the sum of two fp16 numbers, 21 bits or more where it is above 2^-3; numbers below
+// are multiples of 2^-24, 2^-32 of the largest p (one number, 11 bits, put the results of ordinary prompts 0.00028 of their norm
+// off 64 bits, against 0.00021 by the final rounding alone).
 // The results of the first product have the layout that the second takes (a lane holds tokens 4 q + i of one column), and
 // the cache stores values in that order: neither p nor the codes cross lanes.
 #include "fluxbin_kv8_device.h"
@@ -459,11 +461,8 @@ __global__ void __launch_bounds__(512) k_kv8_join(Kv8AttnArgs a) {
 // Prompt chunks. A workgroup takes 16 CT columns for each of its NW wavefronts, of one sequence and head, and goes over all
 // the tokens that they attend. A tile of 64 tokens is decoded once for all wavefronts: each turns a part of its codes into
 // fp16 in LDS, in operand order, a tile ahead of its use, its requests two tiles ahead. Two sequences with 1024 and 700 new
-// rows on 4096 and 1500 tokens, 64 heads of 128 over 8: 243 us, 600 TFLOP/s, 7 of them the launches for sequences of few
-// rows (a large fp16 matrix product: 1144); 4096 rows on 8192 tokens: 820. Counters: matrix cores 24%, vector instructions
-// 40% of the time, the rest waits and uneven ends. 64 columns per wavefront (one per SIMD) took 360 us with the chunks'
-// launch alone, eight wavefronts per workgroup 258, this form 237. p is fed rounded to fp16
-// (its rounding is as large as the result's own; the sum of two numbers as below would be half as much matrix work again).
+// rows on 4096 and 1500 tokens, 64 heads of 128 over 8: 296 us, 495 TFLOP/s, the launches for sequences of few rows among
+// them (a large fp16 matrix product: 1144; with p as one fp16 number, half of the second product's matrix work, 243 us).
 // ---------------------------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ kv_h4 codes4(uint32_t a) {
@@ -637,7 +636,7 @@ __global__ void __launch_bounds__(64 * NW, CT == 4 ? 1 : 2) k_kv8_chunk(Kv8AttnA
             sc[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[c][f], sc[c][j], 0, 0, 0);
           }
         }
-      kv_h8 ph[CT][2];
+      kv_h8 ph[CT][2], pl[CT][2];
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
 #pragma unroll
@@ -678,11 +677,18 @@ __global__ void __launch_bounds__(64 * NW, CT == 4 ? 1 : 2) k_kv8_chunk(Kv8AttnA
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p = __builtin_amdgcn_exp2f(sc[c][j][i]);
+          for (int i = 0; i < 4; i += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(sc[c][j][i]), p1 = __builtin_amdgcn_exp2f(sc[c][j][i + 1]);
             // p before it is rounded: a weight on values of a tiny scale may be lost in p, but not in the sum
-            sum[c] = __builtin_fmaf(p, rj[j], sum[c]);
-            ph[c][j >> 1][4 * (j & 1) + i] = _Float16(p);
+            sum[c] = __builtin_fmaf(p0, rj[j], sum[c]);
+            sum[c] = __builtin_fmaf(p1, rj[j], sum[c]);
+            // the first number cut off (a pair an instruction), the second the rest of it, rounded: 21 bits
+            const kv_h2 up = __builtin_bit_cast(kv_h2, __builtin_amdgcn_cvt_pkrtz(p0, p1));
+            const int at = 4 * (j & 1) + i;
+            ph[c][j >> 1][at] = up.x;
+            ph[c][j >> 1][at + 1] = up.y;
+            pl[c][j >> 1][at] = _Float16(__builtin_fmaf(float(up.x), -1.f, p0));
+            pl[c][j >> 1][at + 1] = _Float16(__builtin_fmaf(float(up.y), -1.f, p1));
           }
       }
 #pragma unroll
@@ -692,6 +698,8 @@ __global__ void __launch_bounds__(64 * NW, CT == 4 ? 1 : 2) k_kv8_chunk(Kv8AttnA
           const kv_h8 v = lv[buf][(j * kE + e) * 64 + lane];
 #pragma unroll
           for (int c = 0; c < CT; ++c) o[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[c][j], o[c][e], 0, 0, 0);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) o[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[c][j], o[c][e], 0, 0, 0);
         }
     }
   }
