@@ -12,7 +12,7 @@ constexpr int kW4MaxBatch = kMaxBatchCall;   // batch rows of one call
 // Row tiles of 16 rows, column chunks of kChunk columns, steps of 4 chunks. Scales (and zero points) come in quads per
 // row: 4 chunks' at one per chunk (group >= 128), 2 chunks' at two, one chunk's at four.
 struct W4Derived {
-  int64_t G;           // groups per row, canonical
+  int64_t g, G;        // columns of a group, at most N; groups per row, canonical
   int64_t Mt, Nc;      // row tiles, chunks
   int gc;              // scales per chunk and row: 1, 2 or 4
   int64_t Nq;          // quads per row
@@ -21,7 +21,8 @@ struct W4Derived {
 
 inline W4Derived w4_derive(const fluxbin_w4_shape& s) {
   W4Derived d{};
-  d.G = ceil_div(s.N, s.g);
+  d.g = s.g < s.N ? s.g : s.N;
+  d.G = ceil_div(s.N, d.g);
   d.Mt = ceil_div(s.M, 16);
   d.Nc = ceil_div(s.N, kChunk);
   d.gc = s.g < kChunk && s.g < s.N ? int(kChunk / s.g) : 1;

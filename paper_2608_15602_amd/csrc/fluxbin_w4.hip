@@ -785,7 +785,7 @@ fluxbin_status launch_w4_pack(const fluxbin_w4_shape& s, const uint32_t* d_codes
                      int32_t(ceil_div(s.N, 8)), int32_t(d.Nc), blocks);
   hipLaunchKernelGGL(k_w4_pack_scales, dim3(unsigned(ceil_div(n, 256))), dim3(256), 0, stream, d_scales, d_zeros,
                      reinterpret_cast<uint16_t*>(base + d.off_scales), s.has_zeros ? base + d.off_zeros : nullptr,
-                     int32_t(s.M), int32_t(s.N), s.g, int32_t(d.G), d.gc, int32_t(d.Nq), n);
+                     int32_t(s.M), int32_t(s.N), d.g, int32_t(d.G), d.gc, int32_t(d.Nq), n);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? FLUXBIN_OK : hip_fail(e, "launching the 4-bit packing");
 }
@@ -807,7 +807,6 @@ fluxbin_status launch_w4_quantize(const void* d_W, int w_is_fp32, int64_t ldw, c
                                   uint32_t* d_codes, uint16_t* d_scales, uint8_t* d_zeros, uint16_t* d_values,
                                   int64_t ldv, hipStream_t stream) {
   const W4Derived d = w4_derive(s);
-  const int64_t g = s.g < s.N ? s.g : s.N;
   const bool split = s.g < 32 || s.g > 512 || (s.g & (s.g - 1)) != 0;   // s.g >= N may be any number
   W4Quant a{};
   a.W = d_W;
@@ -819,7 +818,7 @@ fluxbin_status launch_w4_quantize(const void* d_W, int w_is_fp32, int64_t ldw, c
   a.ldv = ldv;
   a.M = int32_t(s.M);
   a.N = int32_t(s.N);
-  a.g = int32_t(split ? g : s.g);
+  a.g = int32_t(split ? d.g : s.g);
   a.G = int32_t(d.G);
   a.Wn = int32_t(ceil_div(s.N, 8));
   a.per_row = int32_t(split ? d.G : ceil_div(s.N, 512));

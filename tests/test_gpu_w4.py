@@ -244,3 +244,19 @@ def test_quantized_layer_end_to_end(fb):
     mag = x.double().cpu().abs() @ values.double().cpu().abs().T
     assert ((y - ref).abs() <= mag * (2.0 ** -11 + 300 * 2.0 ** -23)).all()
     assert (W.float() - values.float()).abs().max() <= 0.51 * scales.float().max()
+
+
+@pytest.mark.parametrize("M,N", [(40, 300), (5, 3), (2, 1)])
+def test_one_group_of_any_length(fb, M, N):
+    """g far past the row is the same as g = N: codes, scales and products."""
+    import torch
+    log(f"case one group per row M={M} N={N}")
+    W = torch.from_numpy(weights(M, N, seed=11).astype(np.float16)).cuda()
+    x = torch.randn(3, N, device="cuda").half()
+    ref = None
+    for g in (N, 1 << 40, (1 << 63) - 1):
+        codes, scales, zeros, values = fb.fluxbin_w4_quantize(W, g, values=True)
+        got = [codes, scales, zeros, values, fb.fluxbin_w4_gemm(fb.fluxbin_w4_pack(codes, scales, zeros, N, g), x)]
+        assert scales.shape == (M, 1)
+        ref = ref or got
+        assert all(torch.equal(a, b) for a, b in zip(ref, got))

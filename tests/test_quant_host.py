@@ -229,3 +229,13 @@ def test_kv8_no_rows(L):
     """A call without rows is valid and launches nothing."""
     assert _append(L, batch=dict(rows=0), k=None, v=None) == 0
     assert _read(L, batch=dict(rows=0), k=None, v=None) == 0
+
+
+# ---------------------------------------------------------------------------------------------- groups past a row
+
+@pytest.mark.parametrize("g", [1000, 5000, 1 << 40, (1 << 63) - 1])
+def test_w4_one_group_per_row(L, g):
+    """Any g >= N is one group per row, up to the largest number that its type holds: sizes and overlaps count that group."""
+    assert fb.fluxbin_w4_pack_query(_w4(g=g)) == fb.fluxbin_w4_pack_query(_w4(g=1000))
+    assert _quantize(L, shape=_w4(g=g), zeros=A[2] + 599) == INV   # the last scale's second byte
+    assert _pack(L, shape=_w4(g=g), scales=A[3] - 599) == INV
