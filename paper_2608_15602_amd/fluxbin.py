@@ -378,6 +378,14 @@ def _invalid(message: str) -> FluxbinError:
     return FluxbinError(FLUXBIN_ERR_INVALID_ARG, message)
 
 
+def _fits(name: str, value, bits: int = 32) -> int:
+    """ctypes cuts numbers to their field's bits without a word: what does not fit is refused here."""
+    n = int(value)
+    if not -(1 << (bits - 1)) <= n < 1 << (bits - 1):
+        raise _invalid(f"{name} = {n} is out of range")
+    return n
+
+
 def _on_device(device, **tensors) -> None:
     """Launches go to the current device: it must be the operands'."""
     import torch
@@ -427,17 +435,18 @@ def fluxbin_w4_quantize(W, g: int, asymmetric: bool = True, values: bool = False
     import torch
     if W.dim() != 2 or W.dtype not in (torch.float16, torch.float32) or (W.shape[1] > 1 and W.stride(1) != 1):
         raise _invalid("W must be fp16 or fp32 [M, N] with unit inner stride")
-    _on_device(W.device)
     M, N = W.shape
+    g = _fits("g", g, 64)
     if g < 1:
         raise _invalid(f"g = {g} must be >= 1")
+    _on_device(W.device)
     G = -(-N // g)
     use = _Handles()
     new = lambda dtype, *size: use.new(stream, *size, dtype=dtype, device=W.device)
     codes, scales = new(torch.int32, M, -(-N // 8)), new(torch.float16, M, G)
     zeros = new(torch.uint8, M, G) if asymmetric else None
     out = new(torch.float16, M, N) if values else None
-    shape = W4Shape(M, N, int(g), 1 if asymmetric else 0, 0)
+    shape = W4Shape(M, N, g, 1 if asymmetric else 0, 0)
     _check(lib().fluxbin_w4_quantize(ctypes.byref(shape), W.data_ptr(), 1 if W.dtype == torch.float32 else 0,
                                      max(N, W.stride(0)) if M == 1 else W.stride(0), codes.data_ptr(), scales.data_ptr(),
                                      _ptr(zeros), _ptr(out), N, _stream(stream)))
@@ -468,6 +477,7 @@ def fluxbin_w4_pack_query(shape: W4Shape) -> int:
 def fluxbin_w4_pack(codes, scales, zeros, N: int, g: int, stream=None) -> PackedW4:
     """Pack codes, scales and zero points (None: 8 everywhere) as fluxbin_w4_quantize returns them."""
     import torch
+    N, g = _fits("N", N, 64), _fits("g", g, 64)
     if codes.dim() != 2 or g < 1 or N < 1:
         raise _invalid("codes must be int32 [M, ceil(N/8)], N and g at least 1")
     M, G = codes.shape[0], -(-N // g)
@@ -476,7 +486,7 @@ def fluxbin_w4_pack(codes, scales, zeros, N: int, g: int, stream=None) -> Packed
     _dense("scales", scales, torch.float16, (M, G))
     if zeros is not None:
         _dense("zeros", zeros, torch.uint8, (M, G))
-    shape = W4Shape(M, int(N), int(g), 0 if zeros is None else 1, 0)
+    shape = W4Shape(M, N, g, 0 if zeros is None else 1, 0)
     n = fluxbin_w4_pack_query(shape)
     buf = _Handles().new(stream, n, dtype=torch.uint8, device=codes.device)
     out = W4Layer()
@@ -487,7 +497,7 @@ def fluxbin_w4_pack(codes, scales, zeros, N: int, g: int, stream=None) -> Packed
 
 def fluxbin_w4_workspace_query(layer: PackedW4, B: int = 1) -> int:
     n = ctypes.c_size_t(0)
-    _check(lib().fluxbin_w4_workspace_query(layer.ref, int(B), ctypes.byref(n)))
+    _check(lib().fluxbin_w4_workspace_query(layer.ref, _fits("B", B), ctypes.byref(n)))
     return n.value
 
 
@@ -504,7 +514,7 @@ def fluxbin_w4_gemm(layer: PackedW4, x, y=None, out_fp32: bool = False, workspac
     one = x.dim() == 1
     B = 1 if one else x.size(0)
     if x.dtype is not use.half or x.get_device() != index or x.dim() > 2 or x.size(-1) != N or \
-            (N > 1 and x.stride(-1) != 1):
+            (N > 1 and x.stride(-1) != 1) or B > 0x7FFFFFFF:
         raise _invalid(f"x must be fp16 [{N}] or [B, {N}] on {layer.device} with unit inner stride, got {x.dtype} "
                        f"{tuple(x.shape)} on {x.device}")
     if y is None:
@@ -542,7 +552,8 @@ class Kv8Cache:
 
 def fluxbin_kv8_cache_query(pages: int, page_size: int, kv_heads: int, head_dim: int) -> int:
     n = ctypes.c_size_t(0)
-    _check(lib().fluxbin_kv8_cache_query(int(pages), int(page_size), int(kv_heads), int(head_dim), ctypes.byref(n)))
+    _check(lib().fluxbin_kv8_cache_query(_fits("pages", pages, 64), _fits("page_size", page_size), _fits("kv_heads", kv_heads),
+                                         _fits("head_dim", head_dim), ctypes.byref(n)))
     return n.value
 
 
@@ -566,6 +577,8 @@ def _kv8_batch(cache: Kv8Cache, rows: int, offsets, context, block_table) -> Kv8
     if context.size(0) != B or offsets.size(0) != B + 1 or not (context.is_contiguous() and offsets.is_contiguous()) or \
             (blocks > 1 and block_table.stride(1) != 1):
         raise _invalid("offsets must be [B + 1], context [B] (contiguous), block_table [B, blocks] with unit inner stride")
+    if B > 0x7FFFFFFF or blocks > 0x7FFFFFFF:
+        raise _invalid(f"block_table {[B, blocks]} is too large")
     return Kv8Batch(rows, B, blocks, blocks if B == 1 else block_table.stride(0), offsets.data_ptr(), context.data_ptr(),
                     block_table.data_ptr())
 
@@ -595,7 +608,9 @@ def fluxbin_kv8_append(cache: Kv8Cache, k, v, offsets, context, block_table, str
 def fluxbin_kv8_read(cache: Kv8Cache, offsets, context, block_table, rows: int, stream=None):
     """The cached values (k, v), fp16 [rows, kv_heads, head_dim], of the sequences' newest tokens (as fluxbin_kv8_append
     counts them). Rows of no sequence are not written."""
-    use, rows = cache.use, int(rows)
+    use, rows = cache.use, _fits("rows", rows, 64)
+    if rows < 0:
+        raise _invalid(f"rows = {rows} must not be negative")
     b = _kv8_batch(cache, rows, offsets, context, block_table)
     k = use.new(stream, rows, cache.kv_heads, cache.head_dim, dtype=use.half, device=cache.device)
     v = use.new(stream, rows, cache.kv_heads, cache.head_dim, dtype=use.half, device=cache.device)
@@ -607,7 +622,8 @@ def fluxbin_kv8_read(cache: Kv8Cache, offsets, context, block_table, rows: int, 
 
 def fluxbin_kv8_workspace_query(cache: Kv8Cache, rows: int, sequences: int, q_heads: int) -> int:
     n = ctypes.c_size_t(0)
-    _check(lib().fluxbin_kv8_workspace_query(cache.ref, int(rows), int(sequences), int(q_heads), ctypes.byref(n)))
+    _check(lib().fluxbin_kv8_workspace_query(cache.ref, _fits("rows", rows, 64), _fits("sequences", sequences),
+                                             _fits("q_heads", q_heads), ctypes.byref(n)))
     return n.value
 
 
@@ -637,7 +653,7 @@ def fluxbin_kv8_attention(cache: Kv8Cache, q, offsets, context, block_table, out
     status = use.lib.fluxbin_kv8_attention(cache.ref, ctypes.byref(b), heads, q.data_ptr(), q.stride(0), q.stride(1),
                                            out.data_ptr(), out.stride(0), out.stride(1),
                                            cache.head_dim ** -0.5 if scale is None else scale, 1 if causal else 0,
-                                           min(int(window), 0x7FFFFFFF), workspace.data_ptr(), workspace.nbytes,
+                                           max(-1, min(int(window), 0x7FFFFFFF)), workspace.data_ptr(), workspace.nbytes,
                                            use.stream(stream, cache.index))
     if status:
         _check(status)

@@ -239,3 +239,50 @@ def test_w4_one_group_per_row(L, g):
     assert fb.fluxbin_w4_pack_query(_w4(g=g)) == fb.fluxbin_w4_pack_query(_w4(g=1000))
     assert _quantize(L, shape=_w4(g=g), zeros=A[2] + 599) == INV   # the last scale's second byte
     assert _pack(L, shape=_w4(g=g), scales=A[3] - 599) == INV
+
+
+# ---------------------------------------------------------------------------------------------- numbers past the C types
+
+def test_binding_refuses_numbers_that_do_not_fit():
+    """ctypes keeps the low bits of a number: 2^64 + 32 would be 32, with buffers sized for one group per row."""
+    import torch
+    from types import SimpleNamespace
+    h = torch.float16
+    with pytest.raises(fb.FluxbinError, match="g = "):
+        fb.fluxbin_w4_quantize(torch.zeros(4, 64, dtype=h), (1 << 64) + 32)
+    codes, scales = torch.zeros(4, 8, dtype=torch.int32), torch.zeros(4, 1, dtype=h)
+    with pytest.raises(fb.FluxbinError, match="g = "):
+        fb.fluxbin_w4_pack(codes, scales, None, 64, (1 << 64) + 32)
+    with pytest.raises(fb.FluxbinError, match="N = "):
+        fb.fluxbin_w4_pack(codes, scales, None, (1 << 64) + 64, 64)
+    layer = SimpleNamespace(ref=ctypes.byref(_layer()))
+    cache = SimpleNamespace(ref=ctypes.byref(_cache()), index=-1, use=SimpleNamespace(int32=torch.int32, current_device=lambda: -1),
+                            device="meta")
+    for call in (lambda: fb.fluxbin_w4_workspace_query(layer, (1 << 32) + 1),
+                 lambda: fb.fluxbin_kv8_cache_query((1 << 64) + 9, 64, 8, 128), lambda: fb.fluxbin_kv8_cache_query(9, (1 << 32) + 64, 8, 128),
+                 lambda: fb.fluxbin_kv8_cache_query(9, 64, 8 - (1 << 32), 128), lambda: fb.fluxbin_kv8_cache_query(9, 64, 8, 128 + (1 << 40)),
+                 lambda: fb.fluxbin_kv8_workspace_query(cache, 10, (1 << 32) + 1, 8),
+                 lambda: fb.fluxbin_kv8_workspace_query(cache, 10, 1, (1 << 32) + 8),
+                 lambda: fb.fluxbin_kv8_read(cache, None, None, None, (1 << 64) + 1), lambda: fb.fluxbin_kv8_read(cache, None, None, None, -1)):
+        with pytest.raises(fb.FluxbinError) as e:
+            call()
+        assert e.value.status == INV
+    meta = lambda *size: torch.empty(size, dtype=torch.int32, device="meta")   # shapes without memory
+    for B, blocks in (((1 << 32) + 1, 1), (1, (1 << 32) + 5)):
+        with pytest.raises(fb.FluxbinError):
+            fb._kv8_batch(cache, 1, meta(B + 1), meta(B), meta(B, blocks))
+
+
+def test_binding_refuses_windows_that_do_not_fit(monkeypatch):
+    """A negative window is refused however small it is; one past the type is the whole context."""
+    import torch
+    from types import SimpleNamespace
+    seen = []
+    lib = SimpleNamespace(fluxbin_kv8_attention=lambda *a: seen.append(ctypes.c_int32(a[11]).value) or 0)
+    monkeypatch.setattr(fb, "_kv8_rows", lambda cache, name, t, heads: t.size(0))
+    monkeypatch.setattr(fb, "_kv8_batch", lambda *a: fb.Kv8Batch())
+    q = torch.zeros(2, 8, 64)
+    cache = SimpleNamespace(use=SimpleNamespace(lib=lib, stream=lambda *a: None), ref=None, head_dim=64, index=-1, device="cpu")
+    for window in (5, 5 + (1 << 32), -(1 << 32) + 5, -1):
+        fb.fluxbin_kv8_attention(cache, q, None, None, None, out=q, window=window, workspace=torch.zeros(1))
+    assert seen[0] == 5 and seen[1] == (1 << 31) - 1 and seen[2] < 0 and seen[3] < 0
