@@ -512,8 +512,8 @@ def fluxbin_w4_gemm(layer: PackedW4, x, y=None, out_fp32: bool = False, workspac
     M, N, index, use = layer.M, layer.N, layer.index, layer.use
     dtype = use.single if out_fp32 else use.half
     one = x.dim() == 1
-    B = 1 if one else x.size(0)
-    if x.dtype is not use.half or x.get_device() != index or x.dim() > 2 or x.size(-1) != N or \
+    B = x.size(0) if x.dim() == 2 else 1
+    if x.dtype is not use.half or x.get_device() != index or x.dim() not in (1, 2) or x.size(-1) != N or \
             (N > 1 and x.stride(-1) != 1) or B > 0x7FFFFFFF:
         raise _invalid(f"x must be fp16 [{N}] or [B, {N}] on {layer.device} with unit inner stride, got {x.dtype} "
                        f"{tuple(x.shape)} on {x.device}")

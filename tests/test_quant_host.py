@@ -286,3 +286,14 @@ def test_binding_refuses_windows_that_do_not_fit(monkeypatch):
     for window in (5, 5 + (1 << 32), -(1 << 32) + 5, -1):
         fb.fluxbin_kv8_attention(cache, q, None, None, None, out=q, window=window, workspace=torch.zeros(1))
     assert seen[0] == 5 and seen[1] == (1 << 31) - 1 and seen[2] < 0 and seen[3] < 0
+
+
+def test_binding_refuses_scalars():
+    """A tensor without dimensions is refused as one of a wrong shape is."""
+    import torch
+    from types import SimpleNamespace
+    layer = SimpleNamespace(M=300, N=1000, index=-1, device="cpu", use=SimpleNamespace(half=torch.float16, single=torch.float32))
+    with pytest.raises(fb.FluxbinError):
+        fb.fluxbin_w4_gemm(layer, torch.tensor(1.0, dtype=torch.float16))
+    with pytest.raises(fb.FluxbinError):
+        fb.fluxbin_w4_gemm(layer, torch.zeros(1000, dtype=torch.float16), y=torch.tensor(1.0, dtype=torch.float16))
