@@ -220,9 +220,10 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_attention
         for (int f = 0; f < D / 32; ++f) __builtin_memcpy(&qf[f], p + 32 * f + 8 * q4, 16);   // no such column: never stored
       }
       // blocks of 16 tokens 4 (t0 + w) + lane .. of 16 steps: page, key scale with the softmax's, value scale's logarithm
-      // and reciprocal; a block without a page: a logarithm that masks it
+      // and reciprocal; blocks without a page as bits, which are masked as positions are
       int page;
       bool held;
+      uint64_t holes;
       float kf, lv, iv;
       auto look = [&](int w) __attribute__((always_inline)) {   // requests; kf and iv hold what is in the cache
         const int tok = (s.t0 + w) * kTile + 16 * lane;
@@ -235,8 +236,9 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_attention
       };
       auto scales = [&]() __attribute__((always_inline)) {
         const float v = iv > kLeast ? iv : kLeast;
+        holes = __ballot(!held);
         kf = held ? kf * a.scale2 : 0.f;
-        lv = held ? __builtin_amdgcn_logf(v) : -__builtin_inff();
+        lv = __builtin_amdgcn_logf(v);
         iv = __builtin_amdgcn_rcpf(v);
       };
       auto offset = [&](int w, int j) __attribute__((always_inline)) {   // of block j of step w in the codes
@@ -267,6 +269,7 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_attention
       for (int w = w0; w < w1; ++w) {
         const int tok = (s.t0 + w) * kTile;
         float kj[4], lj[4], rj[4];
+        const uint32_t gone = uint32_t(holes >> (((w - w0) & 15) * 4)) & 15u;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int l = ((w - w0) & 15) * 4 + j;
@@ -298,13 +301,13 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_attention
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int i = 0; i < 4; ++i) sc[j][i] = __builtin_fmaf(sc[j][i], kj[j], lj[j]);
-        if (tok < all_lo || tok + kTile > all_hi) {
+        if (tok < all_lo || tok + kTile > all_hi || gone != 0) {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int at = tok + 16 * j + 4 * q4 + i;
-              sc[j][i] = at < hi && at >= lo ? sc[j][i] : -__builtin_inff();
+              sc[j][i] = at < hi && at >= lo && !(gone >> j & 1) ? sc[j][i] : -__builtin_inff();
             }
         }
 #pragma unroll
@@ -461,7 +464,7 @@ __global__ void __launch_bounds__(512) k_kv8_join(Kv8AttnArgs a) {
 // Prompt chunks. A workgroup takes 16 CT columns for each of its NW wavefronts, of one sequence and head, and goes over all
 // the tokens that they attend. A tile of 64 tokens is decoded once for all wavefronts: each turns a part of its codes into
 // fp16 in LDS, in operand order, a tile ahead of its use, its requests two tiles ahead. Two sequences with 1024 and 700 new
-// rows on 4096 and 1500 tokens, 64 heads of 128 over 8: 296 us, 495 TFLOP/s, the launches for sequences of few rows among
+// rows on 4096 and 1500 tokens, 64 heads of 128 over 8: 293 us, 500 TFLOP/s, the launches for sequences of few rows among
 // them (a large fp16 matrix product: 1144; with p as one fp16 number, half of the second product's matrix work, 243 us).
 // ---------------------------------------------------------------------------------------------------------------------
 
@@ -548,8 +551,9 @@ __global__ void __launch_bounds__(64 * NW, CT == 4 ? 1 : 2) k_kv8_chunk(Kv8AttnA
   }
 
   if (t0 < t1) {
-    // blocks of 16 tokens of 16 tiles, one per lane: pages for the requests; scales (a block without a page is masked)
+    // blocks of 16 tokens of 16 tiles, one per lane: pages for the requests; scales; blocks without a page as bits
     int page = 0;
+    uint64_t holes = 0;
     float kf = 0.f, lvs = 0.f, iv = 0.f;
     auto find = [&](int t) __attribute__((always_inline)) {
       const int tok = t * kTile + 16 * lane;
@@ -559,8 +563,9 @@ __global__ void __launch_bounds__(64 * NW, CT == 4 ? 1 : 2) k_kv8_chunk(Kv8AttnA
       const int p = find(t);
       const int64_t at = int64_t(p < 0 ? 0 : p) * a.c.Hkv + head;
       const float ks = a.c.ks[at], vs = a.c.vs[at], v = vs > kLeast ? vs : kLeast;
+      holes = __ballot(p < 0);
       kf = p < 0 ? 0.f : ks * a.scale2;
-      lvs = p < 0 ? -__builtin_inff() : __builtin_amdgcn_logf(v);
+      lvs = __builtin_amdgcn_logf(v);
       iv = __builtin_amdgcn_rcpf(v);
     };
     auto number = [&](float v, int l) __attribute__((always_inline)) {
@@ -617,6 +622,7 @@ __global__ void __launch_bounds__(64 * NW, CT == 4 ? 1 : 2) k_kv8_chunk(Kv8AttnA
       const int tok = t * kTile;
       if (tok >= any_hi || tok + kTile <= any_lo) continue;
       float kj[4], lj[4], rj[4];
+      const uint32_t gone = uint32_t(holes >> (((t - t0) & 15) * 4)) & 15u;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int l = ((t - t0) & 15) * 4 + j;
@@ -645,13 +651,13 @@ __global__ void __launch_bounds__(64 * NW, CT == 4 ? 1 : 2) k_kv8_chunk(Kv8AttnA
 #pragma unroll
           for (int i = 0; i < 4; ++i) sc[c][j][i] = __builtin_fmaf(sc[c][j][i], kj[j], add);
         }
-        if (tok < all_lo || tok + kTile > all_hi) {
+        if (tok < all_lo || tok + kTile > all_hi || gone != 0) {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int at = tok + 16 * j + 4 * q4 + i;
-              sc[c][j][i] = at < hi[c] && at >= lo[c] ? sc[c][j][i] : -__builtin_inff();
+              sc[c][j][i] = at < hi[c] && at >= lo[c] && !(gone >> j & 1) ? sc[c][j][i] : -__builtin_inff();
             }
         }
         float top = -__builtin_inff();

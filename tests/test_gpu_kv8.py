@@ -428,3 +428,28 @@ def test_another_stream(fb):
         side.synchronize()
         assert torch.equal(out, ref)
         assert all(torch.equal(x, y) for x, y in zip((k, v), fb.fluxbin_kv8_read(s.cache, *a, 2)))
+
+
+@pytest.mark.parametrize("new,G,H,D", [([2, 1, 3], 4, 2, 64), ([270, 260, 300], 8, 8, 128), ([270, 260, 300], 8, 8, 256)])
+def test_queries_not_finite_without_pages(fb, new, G, H, D):
+    """NaN and infinities in a query do not come out of blocks without a page: a row whose positions have none is 0, and one
+    beside it with some is as if its own query were alone. Few rows, and as many as the prompt chunks' kernel takes."""
+    import torch
+    log(f"case queries not finite, pages missing, new={new} D={D}")
+    s = Setup(fb, 3, H, D, 32, 320, seed=45)
+    s.append([310, 305, 300])
+    s.table[1, :], s.table[2, :9] = -1, s.pages     # no page; one page of ten
+    offsets = np.concatenate([[0], np.cumsum(new)])
+    q = s.rng.standard_normal((int(offsets[-1]), H * G, D)).astype(np.float16)
+    a = s.arrays(offsets, s.length)
+    good = fb.fluxbin_kv8_attention(s.cache, s.dev(q), *a, causal=False)
+    at = int(offsets[1])
+    assert not good[at:at + new[1]].any() and torch.isfinite(good).all()
+    q[at, 1, 5], q[at, 2, 0], q[at, 3] = np.nan, np.inf, -np.inf
+    bad = fb.fluxbin_kv8_attention(s.cache, s.dev(q), *a, causal=False)
+    assert torch.equal(good, bad)
+    q[int(offsets[2]), 0, 7] = np.nan
+    bad = fb.fluxbin_kv8_attention(s.cache, s.dev(q), *a, causal=False)
+    assert torch.isnan(bad[int(offsets[2]), 0]).all()
+    bad[int(offsets[2]), 0] = good[int(offsets[2]), 0]
+    assert torch.equal(good, bad)
