@@ -461,7 +461,7 @@ __global__ void __launch_bounds__(512) k_kv8_join(Kv8AttnArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Prompt chunks. A workgroup takes 16 CT columns for each of its NW wavefronts, of one sequence and head, and goes over all
+// Prompt chunks. A workgroup takes 16 CT columns for each of its four wavefronts, of one sequence and head, and goes over all
 // the tokens that they attend. A tile of 64 tokens is decoded once for all wavefronts: each turns a part of its codes into
 // fp16 in LDS, in operand order, a tile ahead of its use, its requests two tiles ahead. Two sequences with 1024 and 700 new
 // rows on 4096 and 1500 tokens, 64 heads of 128 over 8: 293 us, 500 TFLOP/s, the launches for sequences of few rows among
@@ -476,10 +476,11 @@ __device__ __forceinline__ kv_h4 codes4(uint32_t a) {
   return kv_h4{x.x, x.y, y.x, y.y};
 }
 
-template <int D, int CT, int NW>
-__global__ void __launch_bounds__(64 * NW, CT == 4 ? 1 : 2) k_kv8_chunk(Kv8AttnArgs a) {
-  constexpr int kCols = 16 * CT * NW, kF = D / 32, kE = D / 16, kU = D / 64;
-  constexpr int kParts = NW / 4;   // wavefronts that share a block of 16 tokens: one does keys and values, or one each
+// D = 256: 128 KB of LDS, one workgroup per CU; otherwise two.
+template <int D, int CT>
+__global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_chunk(Kv8AttnArgs a) {
+  constexpr int kCols = 16 * CT * kWaves, kF = D / 32, kE = D / 16, kU = D / 64;
+  static_assert(kWaves * 16 == kTile, "a block of 16 tokens for each wavefront to decode");
   __shared__ __attribute__((aligned(16))) kv_h8 lk[2][4 * kF * 64], lv[2][2 * kE * 64];   // [block][f][lane], [pair][e][lane]
   const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   const int m16 = lane & 15, q4 = lane >> 4, head = int(blockIdx.y);
@@ -571,33 +572,29 @@ __global__ void __launch_bounds__(64 * NW, CT == 4 ? 1 : 2) k_kv8_chunk(Kv8AttnA
     auto number = [&](float v, int l) __attribute__((always_inline)) {
       return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l));
     };
-    const int block = wave & 3;
-    kv_u4 raw[2 / kParts][kU];
+    kv_u4 raw[2][kU];   // keys, values
     auto request = [&](int t) __attribute__((always_inline)) {   // this wavefront's block of tile t
-      const int tok = t * kTile + 16 * block;
-      const int p = __builtin_amdgcn_readlane(page, ((t - t0) & 15) * 4 + block);
+      const int tok = t * kTile + 16 * wave;
+      const int p = __builtin_amdgcn_readlane(page, ((t - t0) & 15) * 4 + wave);
       const int64_t off = kv_page_offset<D>(a.c, p, head) + int64_t((tok & ((1 << a.c.pshift) - 1)) >> 4) * 16 * D;
 #pragma unroll
-      for (int h = 0; h < 2 / kParts; ++h) {
-        const uint8_t* base = (kParts == 2 ? wave >= 4 : h == 1) ? a.c.v : a.c.k;
+      for (int h = 0; h < 2; ++h) {
+        const uint8_t* base = h == 1 ? a.c.v : a.c.k;
 #pragma unroll
         for (int k = 0; k < kU; ++k) raw[h][k] = *reinterpret_cast<const kv_u4*>(base + off + k * 1024 + uint32_t(lane * 16));
       }
     };
     auto decode = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
-      for (int h = 0; h < 2 / kParts; ++h)
+      for (int k = 0; k < kU; ++k) {
+        lk[buf][(wave * kF + 2 * k) * 64 + lane] = codes8(raw[0][k].x, raw[0][k].y);
+        lk[buf][(wave * kF + 2 * k + 1) * 64 + lane] = codes8(raw[0][k].z, raw[0][k].w);
+      }
 #pragma unroll
-        for (int k = 0; k < kU; ++k) {
-          if (kParts == 2 ? wave < 4 : h == 0) {
-            lk[buf][(block * kF + 2 * k) * 64 + lane] = codes8(raw[h][k].x, raw[h][k].y);
-            lk[buf][(block * kF + 2 * k + 1) * 64 + lane] = codes8(raw[h][k].z, raw[h][k].w);
-          } else {
+      for (int k = 0; k < kU; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              reinterpret_cast<kv_h4*>(&lv[buf][((block >> 1) * kE + 4 * k + e) * 64 + lane])[block & 1] = codes4(raw[h][k][e]);
-          }
-        }
+        for (int e = 0; e < 4; ++e)
+          reinterpret_cast<kv_h4*>(&lv[buf][((wave >> 1) * kE + 4 * k + e) * 64 + lane])[wave & 1] = codes4(raw[1][k][e]);
     };
     auto pages = [&](int t) __attribute__((always_inline)) {
       const int p = find(t);
@@ -727,12 +724,12 @@ int attention_wgs(int cus) { return 2 * cus; }
 // take 1.6 us for every 64 tokens of a long context.
 template <int D>
 void attention_launch(Kv8AttnArgs a, int cus, hipStream_t stream) {
-  constexpr int CT = D == 256 ? 1 : 2, cols = 64 * CT;
+  constexpr int CT = D == 256 ? 1 : 2, cols = 16 * CT * kWaves;
   const int64_t blocks = int64_t(a.c.T) * a.G / cols;
   a.chunk_from = INT32_MAX;
   if (blocks * a.c.Hkv >= cus && blocks >= a.c.B) {
     a.chunk_from = a.c.B > 1 ? cols : 0;
-    hipLaunchKernelGGL((k_kv8_chunk<D, CT, 4>), dim3(unsigned(blocks + a.c.B), unsigned(a.c.Hkv)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((k_kv8_chunk<D, CT>), dim3(unsigned(blocks + a.c.B), unsigned(a.c.Hkv)), dim3(64 * kWaves), 0, stream, a);
     if (a.c.B == 1) return;
   }
   // Short tables: items are not split, which saves the second kernel (2 to 3 us with its launch; 16 tiles are 4 steps for

@@ -6,7 +6,6 @@
 // in fp32. Nothing is rounded to fewer bits before the result.
 #include <type_traits>
 
-
 #include "fluxbin_device.h"
 #include "fluxbin_quant_internal.h"
 
@@ -654,7 +653,7 @@ void launch_gemm_gz(const W4Args& a, int gc, dim3 grid, hipStream_t stream) {
     W4_LAUNCH(1);
   } else if (gc == 2) {
     W4_LAUNCH(2);
-  } else {
+  } else if constexpr (BT == 1 || RT == 1) {   // the plan has no two row tiles there
     W4_LAUNCH(4);
   }
 #undef W4_LAUNCH
