@@ -52,12 +52,16 @@ def w4_dense(codes, scales, zeros, g):
     return (codes.astype(np.int64) - zeros.astype(np.int64)[:, at]) * scales.astype(np.float64)[:, at]
 
 
+def w4_depth(N):
+    """Additions on the longest path of a product's sum: 128 in a group, then one per group, and 32 for the parts of the
+    columns."""
+    return 128 + -(-N // 32) + 32
+
+
 def w4_bound(W, x, half):
     """How far a product may be from W x (fp64 [B, M]): per row one rounding of 2^-23 of the sum of magnitudes for each
-    addition on the longest path (128 in a group, then one per group, and 32 for the parts of the columns); an fp16 result
-    half a step more."""
-    depth = 128 + -(-W.shape[1] // 32) + 32
-    bound = depth * 2.0 ** -23 * (np.abs(x) @ np.abs(W).T)
+    addition on the longest path; an fp16 result half a step more."""
+    bound = w4_depth(W.shape[1]) * 2.0 ** -23 * (np.abs(x) @ np.abs(W).T)
     if half:
         bound = bound * (1 + 2.0 ** -11) + np.abs(x @ W.T) * 2.0 ** -11 + 2.0 ** -25
     return bound
