@@ -725,11 +725,25 @@ W4Plan w4_plan(const fluxbin_w4_shape& s, int B, int cus) {
   return p;
 }
 
+// At least what the plan of any batch up to B needs. Up to 32 rows there are three plans. Past that the times that plans are
+// chosen by change where 32, 48 or 64 more rows begin and, in between, grow with the rows by the parts that are joined: from
+// the first to the last row of such a stretch plans go from more parts to fewer, or to the few-row kernel's.
 uint64_t w4_workspace(const fluxbin_w4_shape& s, int B, int cus) {
   uint64_t most = 0;
-  for (int b = 1; b <= B; ++b) {
-    const uint64_t n = w4_plan(s, b, cus).ws_bytes;
+  auto stretch = [&](int first, int last) {
+    const int a = w4_plan(s, first, cus).parts, b = w4_plan(s, last, cus).parts, parts = a > b ? a : b;
+    const uint64_t n = parts > 1 ? uint64_t(parts) * uint64_t(last) * uint64_t(s.M) * 4u : 0u;
     most = n > most ? n : most;
+  };
+  for (int first = 1; first <= B;) {
+    int last = first <= 4 ? 4 : first <= 16 ? 16 : 32;
+    if (first > 32) {
+      const int to32 = int(ceil_div(first, 32)) * 32, to48 = int(ceil_div(first, 48)) * 48;
+      last = to32 < to48 ? to32 : to48;
+    }
+    if (last > B) last = B;
+    stretch(first, last);
+    first = last + 1;
   }
   return round_up256(most);
 }
