@@ -413,7 +413,9 @@ class _Handles:
         if stream is None:
             return self.empty(size, dtype=dtype, device=device)
         import torch
-        with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))):
+        if not hasattr(stream, "cuda_stream"):   # a handle; that of the null stream is 0, which ExternalStream takes for none
+            stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream(device)
+        with torch.cuda.stream(stream):
             return self.empty(size, dtype=dtype, device=device)
 
     def stream(self, stream, index: int):

@@ -113,3 +113,21 @@ def test_prompts_then_tokens(fb, binary):
         graph.replay()
         torch.cuda.synchronize()
         blk.check(np.arange(B + 1), lengths)
+
+
+def test_memory_of_the_null_stream(fb):
+    """The null stream's handle is 0: what a call on it allocates belongs to that stream, and not to one from torch's pool."""
+    import torch
+    log("case memory of the null stream")
+    n = 1 << 20
+    W = torch.zeros(n, 32, dtype=torch.float16, device="cuda")
+    codes, scales, zeros, values = fb.fluxbin_w4_quantize(W, 32, values=True, stream=0)
+    cache = fb.make_kv8_cache(4, 16, 1, 64)
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    k, v = fb.fluxbin_kv8_read(cache, ints([0, n]), ints([0]), ints([[0]]), n, stream=0)
+    torch.cuda.synchronize()
+    segments = torch.cuda.memory_snapshot()
+    for t in (codes, scales, zeros, values, k, v):
+        where = [s for s in segments if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]]
+        assert len(where) == 1 and where[0]["stream"] == 0
+    assert not values.any() and not k.any() and not v.any()
