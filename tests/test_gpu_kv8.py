@@ -453,3 +453,75 @@ def test_queries_not_finite_without_pages(fb, new, G, H, D):
     assert torch.isnan(bad[int(offsets[2]), 0]).all()
     bad[int(offsets[2]), 0] = good[int(offsets[2]), 0]
     assert torch.equal(good, bad)
+
+
+def test_shared_pages(fb):
+    """Sequences that share their first pages, and one that has a page twice: read and attended by each, while new tokens go
+    to pages of their own."""
+    import torch
+    log("case shared pages")
+    s = Setup(fb, 3, 2, 128, 32, 160, seed=46)
+    s.append([96, 0, 0])
+    s.table[1, :3] = s.table[0, :3]
+    s.table[2, :3] = s.table[0, 1]
+    s.length[:] = 96
+    s.append([20, 1, 40])
+    s.check()
+    s.attend([20, 1, 40], 4)
+    s.attend([1, 1, 1], 4, window=50)
+
+
+def test_two_streams_at_once(fb):
+    """Appends to and attention over different pages of one cache on two streams, each with its workspace, the same captured
+    graphs replayed beside each other, and one replayed twice with other inputs."""
+    import torch
+    log("case two streams")
+    s = Setup(fb, 2, 2, 64, 16, 3000, seed=47)
+    s.append([2900, 2000])
+    q = [s.dev(s.rng.standard_normal((1, 8, 64)).astype(np.float16)) for _ in range(2)]
+    k = [s.dev(s.rng.standard_normal((1, 2, 64)).astype(np.float16)) for _ in range(2)]
+    offsets = s.ints([0, 1])
+    s.length += 1
+    lengths, tables = [s.ints([n]) for n in s.length], [s.ints(s.table[b:b + 1]) for b in range(2)]
+    ws, out = [fb.make_kv8_workspace(s.cache, 1, 1, 8) for _ in range(2)], [torch.zeros_like(x) for x in q]
+
+    def step(b, stream=None):
+        fb.fluxbin_kv8_append(s.cache, k[b], k[b], offsets, lengths[b], tables[b], stream=stream)
+        fb.fluxbin_kv8_attention(s.cache, q[b], offsets, lengths[b], tables[b], out=out[b], workspace=ws[b], stream=stream)
+
+    for b in range(2):
+        step(b)
+    ref = [x.clone() for x in out]
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    for i in range(5):
+        for x in out:
+            x.zero_()
+        torch.cuda.synchronize()
+        for b in range(2):
+            step(b, sides[b])
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(out, ref))
+    graphs = []
+    for b in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[b]):
+            step(b)
+    for i in range(5):
+        for x in out:
+            x.zero_()
+        torch.cuda.synchronize()
+        for g, side in zip(graphs, sides):
+            with torch.cuda.stream(side):
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(out, ref))
+    q[0].neg_()
+    for i in range(3):
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        torch.cuda.synchronize()
+        got = out[0].clone()
+        step(0)
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], got) and not torch.equal(got, ref[0])
