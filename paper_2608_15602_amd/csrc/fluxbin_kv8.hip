@@ -242,24 +242,39 @@ __global__ void __launch_bounds__(256) k_kv8_read(Kv8ReadArgs a, int span) {
   }
 }
 
-// Rows per window: as many as a block or page has where that leaves enough windows, else one (most of which do nothing): a
-// window does its sequences and pages one after another. Reading 880 rows of 32 sequences back, 8 heads, took 10.5 us with
-// windows of 16 rows.
-static int rows_per_window(const Kv8Args& c, int most) {
-  return c.T <= 4 * c.B || int64_t(c.T) * c.Hkv <= 16384 ? 1 : most;
+// Rows per window. A window does its sequences and pages one after another, `each` us a sequence; one that holds no first row
+// of either still has to find that out, `idle` us of the call for each row and windows of one. Batches of nearly only single
+// tokens: one row (append of 32 x 1, 8 heads: 7.8 us, 34 with 8 rows). Many rows: a page's or block's (8192 rows, 8 heads:
+// 14 us, 61 with 8, 298 with 1). In between, the size that is best if every row is a sequence of its own: append of 2048 rows,
+// 8 heads, as one sequence 8.6 us with a page's 64, 33 with 4, 79 with 1; as 32 sequences 8.6, 34 and 85; as one of 2000 and
+// 31 single tokens 129, 29 and 38; reading them back with 16, 4 and 1 rows 9.0, 10.1 and 22; 8.9, 10.4 and 23; 32, 15 and 13.
+static int rows_per_window(const Kv8Args& c, int most, double each, double idle) {
+  if (c.T <= 4 * c.B) return 1;
+  if (int64_t(c.T) * c.Hkv > 16384) return most;
+  int best = 1;
+  double least = 0;
+  for (int span = 1; span <= most; span *= 2) {
+    const double us = each * (span < c.B ? span : c.B) + idle * c.T / span;
+    if (span == 1 || us < least) {
+      best = span;
+      least = us;
+    }
+  }
+  return best;
 }
 
+// Two heads a workgroup where windows are long: four prompts of 301 to 2000 tokens, 40 heads, 44 us; 49 with one, 47.5 with four.
 template <int D>
 void append_launch(const Kv8AppendArgs& a, hipStream_t stream) {
-  const int span = rows_per_window(a.c, 1 << a.c.pshift), heads = span > 1 ? 2 : 1;
+  const int span = rows_per_window(a.c, 1 << a.c.pshift, 4.0, a.c.Hkv / 225.0), heads = span > 1 ? 2 : 1;
   const dim3 grid(unsigned(ceil_div(a.c.T, span)), unsigned(ceil_div(a.c.Hkv, heads)), 2);
   hipLaunchKernelGGL(k_kv8_append<D>, grid, dim3(256), 0, stream, a, span, heads);
 }
 
 template <int D>
 void read_launch(const Kv8ReadArgs& a, hipStream_t stream) {
-  const int span = rows_per_window(a.c, 16);
-  const dim3 grid(unsigned(ceil_div(a.c.T, span)), unsigned(ceil_div(a.c.Hkv, 4)), 2);
+  const int quads = int(ceil_div(a.c.Hkv, 4)), span = rows_per_window(a.c, 16, 1.8, quads / 325.0);
+  const dim3 grid(unsigned(ceil_div(a.c.T, span)), unsigned(quads), 2);
   hipLaunchKernelGGL(k_kv8_read<D>, grid, dim3(256), 0, stream, a, span);
 }
 

@@ -525,3 +525,17 @@ def test_two_streams_at_once(fb):
         step(0)
         torch.cuda.synchronize()
         assert torch.equal(out[0], got) and not torch.equal(got, ref[0])
+
+
+@pytest.mark.parametrize("H,P,new", [
+    (8, 64, [700]), (2, 16, [333, 1000]), (8, 32, [1] * 7 + [500] + [1] * 8), (3, 128, [5] * 40), (8, 64, [17] * 30),
+    (1, 256, [1] * 20 + [3000, 0, 0] + [2] * 9), (40, 16, [9] * 12 + [250]), (1, 64, [1, 900, 1, 800])])
+def test_append_windows(fb, H, P, new):
+    """Calls of every number of rows per window between one and a page's: one prompt, several, single tokens beside one."""
+    log(f"case windows H={H} P={P} new={new}")
+    s = Setup(fb, len(new), H, 64, P, max(new) + 40, seed=48)
+    s.append([b % 37 for b in range(len(new))])
+    s.append(new, 2.0)
+    s.check()
+    s.append([n % 3 for n in new], 3.0)
+    s.check()
