@@ -1,8 +1,8 @@
 // Paged key/value cache in 8 bits: storing new tokens and reading them back.
 //
 // Both are bound by memory where there is much to do: storing four prompts of 301 to 2000 tokens, 40 heads of 128, from rows of
-// a fused projection 51 us (126 MB; 42 us from dense rows), reading them back 25.5 us (145 MB, 5.7 TB/s). A single token of 32
-// sequences is 4 us: five requests one after another (sequence, lengths, page, values, scale).
+// a fused projection 50 us (126 MB; 42 us from dense rows), reading them back 25.5 us (145 MB, 5.7 TB/s). A single token of 32
+// sequences is 4.2 to 5.3 us under the profiler: five requests one after another (sequence, lengths, page, values, scale).
 #include "fluxbin_kv8_device.h"
 
 namespace fluxbin {
@@ -247,13 +247,14 @@ __global__ void __launch_bounds__(256) k_kv8_read(Kv8ReadArgs a, int span) {
 // tokens: one row (append of 32 x 1, 8 heads: 7.8 us, 34 with 8 rows). Many rows: a page's or block's (8192 rows, 8 heads:
 // 14 us, 61 with 8, 298 with 1). In between, the size that is best if every row is a sequence of its own: append of 2048 rows,
 // 8 heads, as one sequence 8.6 us with a page's 64, 33 with 4, 79 with 1; as 32 sequences 8.6, 34 and 85; as one of 2000 and
-// 31 single tokens 129, 29 and 38; reading them back with 16, 4 and 1 rows 9.0, 10.1 and 22; 8.9, 10.4 and 23; 32, 15 and 13.
-static int rows_per_window(const Kv8Args& c, int most, double each, double idle) {
+// 31 single tokens 129, 29 and 38; reading them back with 16, 4 and 1 rows 9.0, 10.1 and 22; 8.9, 10.4 and 23; 32, 15 and 13
+// (2 rows 16: sizes go up by `by`).
+static int rows_per_window(const Kv8Args& c, int most, int by, double each, double idle) {
   if (c.T <= 4 * c.B) return 1;
   if (int64_t(c.T) * c.Hkv > 16384) return most;
   int best = 1;
   double least = 0;
-  for (int span = 1; span <= most; span *= 2) {
+  for (int span = 1; span <= most; span *= by) {
     const double us = each * (span < c.B ? span : c.B) + idle * c.T / span;
     if (span == 1 || us < least) {
       best = span;
@@ -266,14 +267,14 @@ static int rows_per_window(const Kv8Args& c, int most, double each, double idle)
 // Two heads a workgroup where windows are long: four prompts of 301 to 2000 tokens, 40 heads, 44 us; 49 with one, 47.5 with four.
 template <int D>
 void append_launch(const Kv8AppendArgs& a, hipStream_t stream) {
-  const int span = rows_per_window(a.c, 1 << a.c.pshift, 4.0, a.c.Hkv / 225.0), heads = span > 1 ? 2 : 1;
+  const int span = rows_per_window(a.c, 1 << a.c.pshift, 2, 4.0, a.c.Hkv / 225.0), heads = span > 1 ? 2 : 1;
   const dim3 grid(unsigned(ceil_div(a.c.T, span)), unsigned(ceil_div(a.c.Hkv, heads)), 2);
   hipLaunchKernelGGL(k_kv8_append<D>, grid, dim3(256), 0, stream, a, span, heads);
 }
 
 template <int D>
 void read_launch(const Kv8ReadArgs& a, hipStream_t stream) {
-  const int quads = int(ceil_div(a.c.Hkv, 4)), span = rows_per_window(a.c, 16, 1.8, quads / 325.0);
+  const int quads = int(ceil_div(a.c.Hkv, 4)), span = rows_per_window(a.c, 16, 4, 1.8, quads / 500.0);
   const dim3 grid(unsigned(ceil_div(a.c.T, span)), unsigned(quads), 2);
   hipLaunchKernelGGL(k_kv8_read<D>, grid, dim3(256), 0, stream, a, span);
 }

@@ -464,8 +464,10 @@ __global__ void __launch_bounds__(512) k_kv8_join(Kv8AttnArgs a) {
 // Prompt chunks. A workgroup takes 16 CT columns for each of its four wavefronts, of one sequence and head, and goes over all
 // the tokens that they attend. A tile of 64 tokens is decoded once for all wavefronts: each turns a part of its codes into
 // fp16 in LDS, in operand order, a tile ahead of its use, its requests two tiles ahead. Two sequences with 1024 and 700 new
-// rows on 4096 and 1500 tokens, 64 heads of 128 over 8: 293 us, 500 TFLOP/s, the launches for sequences of few rows among
-// them (a large fp16 matrix product: 1144; with p as one fp16 number, half of the second product's matrix work, 243 us).
+// rows on 4096 and 1500 tokens, 64 heads of 128 over 8: 292 us, 500 TFLOP/s, the launches for sequences of few rows among
+// them (a large fp16 matrix product: 1144; with p as one fp16 number, half of the second product's matrix work, 243 us); 4096
+// rows on 8192 tokens 716. Counters: matrix cores 30%, vector instructions 38% of the SIMDs' time, wavefronts wait 21% of
+// theirs and fill 59% of their places: the rest is uneven ends.
 // ---------------------------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ kv_h4 codes4(uint32_t a) {
@@ -719,9 +721,13 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_chunk(Kv8
 
 int attention_wgs(int cus) { return 2 * cus; }
 
-// Prompt chunks where they fill the chip: a workgroup of four wavefronts, 32 columns each (16 for D = 256). Sequences with
-// fewer rows than one workgroup's columns among them go to the other kernel, which splits their tokens: one workgroup would
-// take 1.6 us for every 64 tokens of a long context.
+// Prompt chunks where their workgroups (four wavefronts of 32 columns each, 16 for D = 256) are one per CU at least: fresh
+// causal prompts of 64 heads over 8, 128 / 256 / 512 rows 10.6 / 14.7 / 24 us, by the other kernel 8.6 / 15.8 / 40; of 32 heads
+// over 32, 512 / 1000 / 1024 rows 22 / 37 / 45 and 21 / 81 / 62; of 8 over 1, 2048 / 4096 rows 66 / 127 and 54 / 185; 256 / 512
+// rows of 64 over 8 on 8192 tokens 250 / 350 and 163 / 320 (few workgroups and long contexts: the other kernel splits them).
+// And where sequences have on average as many columns as a workgroup: 64 of 12 rows, 64 heads over 8, 37 us and 34; of 16 rows
+// 20 and 44. Sequences with fewer columns than one workgroup's among them go to the other kernel, which splits their
+// tokens: one workgroup would take 2 us for every 64 tokens of a long context.
 template <int D>
 void attention_launch(Kv8AttnArgs a, int cus, hipStream_t stream) {
   constexpr int CT = D == 256 ? 1 : 2, cols = 16 * CT * kWaves;
@@ -732,8 +738,8 @@ void attention_launch(Kv8AttnArgs a, int cus, hipStream_t stream) {
     hipLaunchKernelGGL((k_kv8_chunk<D, CT>), dim3(unsigned(blocks + a.c.B), unsigned(a.c.Hkv)), dim3(64 * kWaves), 0, stream, a);
     if (a.c.B == 1) return;
   }
-  // Short tables: items are not split, which saves the second kernel (2 to 3 us with its launch; 16 tiles are 4 steps for
-  // each of a workgroup's wavefronts).
+  // Short tables: items are not split, which saves the second kernel. Single tokens of up to 900 / 1800 tokens, whole and split:
+  // one sequence of 32 heads 10.8 / 16 and 13.6 / 14 us, 8 of 64 heads over 8 11 / 16.5 and 14.7 / 17.
   a.whole = (int64_t(a.c.max_blocks) << a.c.pshift) <= 15 * kTile;
   // Single tokens of groups of up to 16 heads: 32 sequences of 256 to 8192 tokens 42.5 us with streaming requests, 45 without,
   // 4 of 16384 with 40 heads 109 and 121; eight tokens of 8 sequences of 8192 (four column tiles) 56.7 and 55.3.

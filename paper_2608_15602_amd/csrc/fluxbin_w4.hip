@@ -187,7 +187,10 @@ __global__ void __launch_bounds__(256) k_w4_pack_scales(const uint16_t* scales, 
 // four whole row pieces of 256 bytes (XR requests a chunk), and lanes pick their operands from there: straight from memory
 // an operand is 64 bytes of each of 16 rows, and such requests took 2.5 times as long and bound the kernel (8192x28672 at
 // B = 16: 65 us with them). 28672x8192 with zero points per group of 128 at B = 1: 29 us (122 MB, 4.2 TB/s; the kernel
-// alone 24.5, 5.0 TB/s); 8192x28672 at B = 16: 37 us; 4096x4096 at B = 1: 5 us.
+// under the profiler 24.9); 8192x28672 at B = 16: 37 us; 4096x4096 at B = 1: 5 us.
+// Activations are handed over inside a wavefront: its LDS operations happen in the order in which they are issued, and the
+// compiler keeps a store and a load that may meet in order. No fences: with one on either side of each store 28672x8192 at
+// B = 1 took 36.6 us (8192x28672 at B = 16: 33.6).
 // ---------------------------------------------------------------------------------------------------------------------
 
 // Eight activations from column c of a row, zero past its end: the requests go out together, past the end for the last
@@ -427,7 +430,7 @@ __global__ void __launch_bounds__(64 * NW) k_w4_gemm(W4Args a) {
 // scales come as far ahead into registers. At the end the halves' sums are added in LDS; with more parts a second kernel
 // adds the parts' sums. Bound by the vector work and the matrix cores beside it about equally (8192x8192 at B = 512:
 // 39% and 31% of the time, the rest waits), so two wavefronts share a SIMD. 11008x4096 with groups of 64 at B = 256: 50 us,
-// 460 TFLOP/s on 172 workgroups for 256 CUs; 28672x8192 at B = 512: 318 us, 760 TFLOP/s.
+// 460 TFLOP/s on 172 workgroups for 256 CUs; 28672x8192 at B = 512: 313 us, 770 TFLOP/s; 8192x8192 at B = 2048: 886.
 // ---------------------------------------------------------------------------------------------------------------------
 
 template <int NB, int GC, bool ZERO>
