@@ -30,8 +30,9 @@ SOURCES = ["fluxbin_host.cpp", "fluxbin_pack.hip", "fluxbin_gemv.hip", "fluxbin_
            "fluxbin_gemm_mfma.hip", "fluxbin_rc.hip", "fluxbin_noalloc.hip",
            "fluxbin_gemv_rows.hip", "fluxbin_gemm_mfma_rows.hip", "fluxbin_gemm_mx.hip",
            "fluxbin_gemm_prefill.hip", "fluxbin_quant_host.cpp", "fluxbin_w4.hip",
-           "fluxbin_kv8.hip", "fluxbin_kv8_attention.hip"]
-HOST_SOURCES = ("fluxbin_host.cpp", "fluxbin_quant_host.cpp")   # what --host-sanitizers instruments
+           "fluxbin_kv8.hip", "fluxbin_kv8_attention.hip", "fluxbin_serve_host.cpp", "fluxbin_rotate.hip",
+           "fluxbin_tree.hip", "fluxbin_kv8_keep.hip", "fluxbin_pages.hip"]
+HOST_SOURCES = ("fluxbin_host.cpp", "fluxbin_quant_host.cpp", "fluxbin_serve_host.cpp")   # what --host-sanitizers instruments
 ARCH = "gfx950"
 
 # Packed-FP32 instructions are kept out of the generated code (plain float code only).

@@ -45,11 +45,6 @@ __device__ __forceinline__ uint32_t kv_code4(uint16_t a, uint16_t b, uint16_t c,
   return lo | hi;
 }
 
-// An earlier token's code after its page's scale has grown.
-__device__ __forceinline__ uint32_t kv_recode(uint32_t byte, float ratio) {
-  return uint32_t(int(__builtin_rintf(float(int(byte) - 128) * ratio)) + 128);
-}
-
 constexpr int kSlab = 64;   // tokens that are staged in LDS at a time (units straight from memory, two bytes of sixteen
                             // places each, took four times as long)
 

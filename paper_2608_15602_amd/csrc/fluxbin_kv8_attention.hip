@@ -11,6 +11,7 @@
 // The results of the first product have the layout that the second takes (a lane holds tokens 4 q + i of one column), and
 // the cache stores values in that order: neither p nor the codes cross lanes.
 #include "fluxbin_kv8_device.h"
+#include "fluxbin_serve_internal.h"
 
 namespace fluxbin {
 
@@ -39,16 +40,19 @@ struct Seq {
   int qt, t0, nt;              // column tiles, first token tile, token tiles
 };
 
+template <bool TREE>
 __device__ __forceinline__ Seq seq_of(const Kv8AttnArgs& a, int b) {
   Seq s;
   const int o0 = a.c.offsets[b], o1 = a.c.offsets[b + 1];
   s.start = o0;
   s.n = o0 >= 0 && o1 <= a.c.T && o1 > o0 ? o1 - o0 : 0;
+  if (TREE && s.n > 64 * a.words) s.n = 0;
   s.ctx = kv_context(a.c, b);
   const int cap = a.c.max_blocks << a.c.pshift;
   s.end = s.ctx < cap ? s.ctx : cap;
   int begin = 0;
-  if (a.window > 0 && s.ctx - s.n + 1 > a.window) begin = s.ctx - s.n + 1 - a.window;
+  // of a tree, a row may attend only cached tokens
+  if (a.window > 0 && s.ctx - s.n + (TREE ? 0 : 1) > a.window) begin = s.ctx - s.n + (TREE ? 0 : 1) - a.window;
   if (begin > s.end) begin = s.end;
   s.qt = s.n * a.G >= a.chunk_from ? 0 : (s.n * a.G + 15) >> 4;   // the others are the prompt chunks' kernel's
   s.t0 = begin / kTile;
@@ -72,6 +76,7 @@ __device__ __forceinline__ int64_t quotient(int64_t v, int by) {   // v >= 0, by
 }
 
 // The sequences of a call as a wavefront sees them: 64 at a time, one per lane.
+template <bool TREE>
 struct Walk {
   const Kv8AttnArgs& a;
   int lane, base;     // the lanes hold sequences base ..
@@ -83,7 +88,7 @@ struct Walk {
 
   __device__ __forceinline__ void load() {
     const int b = base + lane;
-    mine = seq_of(a, b < a.c.B ? b : a.c.B - 1);
+    mine = seq_of<TREE>(a, b < a.c.B ? b : a.c.B - 1);
     if (b >= a.c.B) mine.qt = 0;
     int64_t v = units_of(a, mine);
     for (int o = 1; o < 64 && o < a.c.B; o <<= 1) {   // lanes past the last sequence: not whole sums
@@ -100,7 +105,7 @@ struct Walk {
   __device__ __forceinline__ int64_t total() {
     int64_t sum = uniform64(__shfl(upto, a.c.B < 64 ? a.c.B - 1 : 63));
     for (int b = 64 + lane; b - lane < a.c.B; b += 64) {
-      int64_t v = b < a.c.B ? units_of(a, seq_of(a, b)) : 0;
+      int64_t v = b < a.c.B ? units_of(a, seq_of<TREE>(a, b)) : 0;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
       sum += uniform64(v);
@@ -132,6 +137,38 @@ struct Walk {
     return s;
   }
 };
+
+// Of a row's mask: bits `from` .. from + 63 of a tree of n rows, with the positions before the tree (negative) set.
+__device__ __forceinline__ uint64_t tree_bits(const uint64_t* mask, int words, int from, int n) {
+  if (from <= -64) return ~uint64_t(0);
+  if (from >= n) return 0;
+  const int w = from >> 6, sh = from & 63;   // w = -1: the word before the tree's
+  const uint64_t lo = w < 0 ? ~uint64_t(0) : mask[w], hi = w + 1 < words ? mask[w + 1] : 0;
+  uint64_t v = sh ? (lo >> sh) | (hi << (64 - sh)) : lo;
+  if (n - from < 64) v &= (uint64_t(1) << (n - from)) - 1;
+  return v;
+}
+
+// The first position that a row attends: with a window, its last attended ones from there on are `window`, those of the tree
+// counted by its mask.
+__device__ __forceinline__ int tree_low(const Kv8AttnArgs& a, const uint64_t* mask, int fresh, int n) {
+  if (a.window <= 0) return 0;
+  int left = a.window;
+  for (int w = (n - 1) >> 6; w >= 0; --w) {
+    uint64_t v = tree_bits(mask, a.words, 64 * w, n);
+    if (fresh < 0) {   // positions below 0 are nobody's
+      const int below = -fresh - 64 * w;
+      v = below >= 64 ? 0 : below > 0 ? v & (~uint64_t(0) << below) : v;
+    }
+    const int bits = __popcll((unsigned long long)v);
+    if (bits >= left) {
+      for (int i = bits; i > left; --i) v &= v - 1;
+      return fresh + 64 * w + __ffsll((unsigned long long)v) - 1;
+    }
+    left -= bits;
+  }
+  return fresh > left ? fresh - left : 0;
+}
 
 // Units per workgroup: an even share, at least one step for each wavefront.
 __device__ __forceinline__ int64_t quota_of(const Kv8AttnArgs& a, int64_t total) {
@@ -173,13 +210,14 @@ __device__ __forceinline__ void store_out(const Kv8AttnArgs& a, const Seq& s, in
 // 50 us, 4.7 TB/s, 6 of them the join; 32 of 256 to 8192 tokens: 43 us, 3.6 TB/s, where a workgroup's share is 18 steps of
 // one or two items and every item's start (lengths, pages, codes, one after another) is seen.
 // ONCE: every code is read by one workgroup only (one column tile), past the caches' ordinary order.
-template <int D, bool ONCE>
+// TREE: rows attend what is before their sequence's first, and of its rows those that their masks name.
+template <int D, bool ONCE, bool TREE>
 __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_attention(Kv8AttnArgs a) {
   __shared__ __attribute__((aligned(16))) float lds_o[kWaves][16][D + 4];
   __shared__ float lds_m[kWaves][16], lds_l[kWaves][16];
   const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   const int m16 = lane & 15, q4 = lane >> 4;
-  Walk walk(a);
+  Walk<TREE> walk(a);
   const int64_t total = walk.total(), quota = quota_of(a, total);
   const int64_t u0 = quota * blockIdx.x;
   const int64_t u1 = u0 + quota < total ? u0 + quota : total;
@@ -197,13 +235,24 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_attention
 
     const int col = ct * 16 + m16, ci = col / a.G, cg = col - ci * a.G;   // this lane's column
     const bool has = ci < s.n;
-    const int pos = s.ctx - s.n + ci;
+    const int pos = s.ctx - s.n + ci, fresh = s.ctx - s.n;   // position of the sequence's first row
+    const uint64_t* mask = TREE ? a.masks + int64_t(s.start + (has ? ci : 0)) * a.words : nullptr;
     const int hi = has ? (a.causal && pos + 1 < s.end ? pos + 1 : s.end) : 0;
-    const int lo = a.window > 0 && pos + 1 > a.window ? pos + 1 - a.window : 0;
+    const int lo = TREE ? tree_low(a, mask, fresh, s.n) : a.window > 0 && pos + 1 > a.window ? pos + 1 - a.window : 0;
     // tokens that all of the tile's columns attend
     const int i0 = ct * 16 / a.G, i1 = (ct * 16 + 15) / a.G, il = i1 < s.n ? i1 : s.n - 1;
-    const int all_hi = a.causal && s.ctx - s.n + i0 + 1 < s.end ? s.ctx - s.n + i0 + 1 : s.end;
-    const int all_lo = a.window > 0 && s.ctx - s.n + il + 1 > a.window ? s.ctx - s.n + il + 1 - a.window : 0;
+    int all_hi = a.causal && s.ctx - s.n + i0 + 1 < s.end ? s.ctx - s.n + i0 + 1 : s.end;
+    int all_lo = a.window > 0 && s.ctx - s.n + il + 1 > a.window ? s.ctx - s.n + il + 1 - a.window : 0;
+    if (TREE) {
+      all_hi = fresh < s.end ? fresh : s.end;
+      all_lo = lo;
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) {
+        const int other = __shfl_xor(all_lo, o);
+        all_lo = other > all_lo ? other : all_lo;
+      }
+      all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    }
 
     kv_f4 o[D / 16];
 #pragma unroll
@@ -302,12 +351,15 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_attention
 #pragma unroll
           for (int i = 0; i < 4; ++i) sc[j][i] = __builtin_fmaf(sc[j][i], kj[j], lj[j]);
         if (tok < all_lo || tok + kTile > all_hi || gone != 0) {
+          const uint64_t seen = TREE ? tree_bits(mask, a.words, tok - fresh, s.n) : 0;
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int at = tok + 16 * j + 4 * q4 + i;
-              sc[j][i] = at < hi && at >= lo && !(gone >> j & 1) ? sc[j][i] : -__builtin_inff();
+              bool in = at < hi && at >= lo && !(gone >> j & 1);
+              if (TREE) in = in && (seen >> (16 * j + 4 * q4 + i) & 1);
+              sc[j][i] = in ? sc[j][i] : -__builtin_inff();
             }
         }
 #pragma unroll
@@ -512,7 +564,7 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_chunk(Kv8
     }
     cb -= __builtin_amdgcn_readlane(upto, 63);
   }
-  const Seq s = seq_of(a, b);
+  const Seq s = seq_of<false>(a, b);
   const int first_pos = s.ctx - s.n;
   const int i_lo = cb * kCols / a.G, i_hi0 = (cb * kCols + kCols - 1) / a.G, i_hi = i_hi0 < s.n ? i_hi0 : s.n - 1;
   int end = a.causal && first_pos + i_hi + 1 < s.end ? first_pos + i_hi + 1 : s.end;
@@ -744,13 +796,35 @@ void attention_launch(Kv8AttnArgs a, int cus, hipStream_t stream) {
   // Single tokens of groups of up to 16 heads: 32 sequences of 256 to 8192 tokens 42.5 us with streaming requests, 45 without,
   // 4 of 16384 with 40 heads 109 and 121; eight tokens of 8 sequences of 8192 (four column tiles) 56.7 and 55.3.
   if (a.c.T <= a.c.B && a.G <= 16)
-    hipLaunchKernelGGL((k_kv8_attention<D, true>), dim3(unsigned(a.wgs)), dim3(64 * kWaves), 0, stream, a);
+    hipLaunchKernelGGL((k_kv8_attention<D, true, false>), dim3(unsigned(a.wgs)), dim3(64 * kWaves), 0, stream, a);
   else
-    hipLaunchKernelGGL((k_kv8_attention<D, false>), dim3(unsigned(a.wgs)), dim3(64 * kWaves), 0, stream, a);
+    hipLaunchKernelGGL((k_kv8_attention<D, false, false>), dim3(unsigned(a.wgs)), dim3(64 * kWaves), 0, stream, a);
+  if (!a.whole) hipLaunchKernelGGL(k_kv8_join<D>, dim3(unsigned(a.wgs - 1), 4), dim3(512), 0, stream, a);
+}
+
+template <int D>
+void tree_launch(Kv8AttnArgs a, hipStream_t stream) {
+  a.chunk_from = INT32_MAX;
+  a.whole = (int64_t(a.c.max_blocks) << a.c.pshift) <= 15 * kTile;
+  hipLaunchKernelGGL((k_kv8_attention<D, false, true>), dim3(unsigned(a.wgs)), dim3(64 * kWaves), 0, stream, a);
   if (!a.whole) hipLaunchKernelGGL(k_kv8_join<D>, dim3(unsigned(a.wgs - 1), 4), dim3(512), 0, stream, a);
 }
 
 }  // namespace
+
+uint64_t kv8_tree_workspace(int32_t D, int cus) { return kv8_workspace(D, cus); }
+
+fluxbin_status launch_kv8_tree_attention(Kv8AttnArgs a, int D, int cus, hipStream_t stream) {
+  a.wgs = attention_wgs(cus);
+  if (D == 64)
+    tree_launch<64>(a, stream);
+  else if (D == 128)
+    tree_launch<128>(a, stream);
+  else
+    tree_launch<256>(a, stream);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? FLUXBIN_OK : hip_fail(e, "launching the attention of trees");
+}
 
 uint64_t kv8_workspace(int32_t D, int cus) {
   return round_up256(uint64_t(attention_wgs(cus)) * (2u * uint64_t(16 * D + 32) * 4u + sizeof(Joint)));

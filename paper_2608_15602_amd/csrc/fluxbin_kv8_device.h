@@ -52,6 +52,11 @@ __device__ __forceinline__ int kv_context(const Kv8Args& a, int b) {
   return c < 0 ? 0 : c > (1 << 30) ? 1 << 30 : c;
 }
 
+// An earlier token's code after its page's scale has grown.
+__device__ __forceinline__ uint32_t kv_recode(uint32_t byte, float ratio) {
+  return uint32_t(int(__builtin_rintf(float(int(byte) - 128) * ratio)) + 128);
+}
+
 // The page of a position of sequence b, or -1.
 __device__ __forceinline__ int kv_page(const Kv8Args& a, int b, int pos) {
   const int p = pos >> a.pshift;

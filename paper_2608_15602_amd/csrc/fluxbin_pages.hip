@@ -1,0 +1,310 @@
+// Pages of the paged 8-bit cache: who holds which, and copies of them.
+//
+// A page is free if its count of references is 0, and free pages are taken lowest number first, so that the outcome depends on
+// the counts alone: counts are changed by integer atomics, whose order does not matter, and one workgroup takes pages, for the
+// sequences in order.
+#include "fluxbin_device.h"
+#include "fluxbin_serve_internal.h"
+
+namespace fluxbin {
+
+namespace {
+
+typedef int pg_i4 __attribute__((ext_vector_type(4)));
+
+constexpr int kTake = 1024;   // threads of the workgroup that takes pages
+
+__device__ __forceinline__ bool is_page(int page, int pages) { return page >= 0 && page < pages; }
+
+// Inclusive sums over a workgroup's threads; total in every thread.
+__device__ __forceinline__ int block_sum(int v, int* red, int& total) {
+  const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(v, o);
+    if (lane >= o) v += u;
+  }
+  __syncthreads();   // red of the sum before
+  if (lane == 63) red[wave] = v;
+  __syncthreads();
+  total = 0;
+  for (int w = 0; w < kTake / 64; ++w) {
+    const int s = red[w];
+    if (w < wave) v += s;
+    total += s;
+  }
+  return v;
+}
+
+// Takes free pages for the wants of up to kTake rows, in order: `want` entries of this thread's row, from entry `from` of `row`
+// on. scan: the page from which on to look, the same in all threads. Returns how many pages were missing, in all threads.
+// copies, source: where not NULL, (source, page) of this thread's one want.
+struct Taking {
+  int want, from;
+  int32_t* row;
+  int32_t* copies;
+  int source;
+};
+
+struct TakeLds {
+  int red[kTake / 64];
+  int upto[kTake];
+  Taking who[kTake];
+  int next;
+};
+
+__device__ int take(const PoolArgs& p, const Taking& mine, int& scan, TakeLds& s) {
+  const int tid = int(threadIdx.x);
+  int wanted;
+  const int upto = block_sum(mine.want, s.red, wanted);
+  s.upto[tid] = upto;
+  s.who[tid] = mine;
+  __syncthreads();
+  int32_t* refs = p.state + 4;
+  int done = 0;
+  while (done < wanted && scan < p.pages) {
+    // four counts a thread; others may raise counts of pages in use meanwhile, not of free ones
+    const int at = (scan & ~3) + 4 * tid;
+    pg_i4 r = {1, 1, 1, 1};
+    if (at + 3 < p.pages) {
+      r = *reinterpret_cast<const pg_i4*>(refs + at);
+    } else {
+      for (int i = 0; i < 4; ++i)
+        if (at + i < p.pages) r[i] = refs[at + i];
+    }
+    int free = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (at + i < scan) r[i] = 1;
+      free += r[i] <= 0 ? 1 : 0;
+    }
+    int found;
+    int k = done + block_sum(free, s.red, found) - free;
+    if (tid == 0) s.next = (scan & ~3) + 4 * kTake;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (r[i] > 0) continue;
+      if (k < wanted) {
+        int lo = 0, n = kTake;   // the first row whose sum is above k
+        while (n > 0) {
+          const int h = n >> 1;
+          if (s.upto[lo + h] <= k) {
+            lo += h + 1;
+            n -= h + 1;
+          } else {
+            n = h;
+          }
+        }
+        const Taking& w = s.who[lo];
+        const int e = w.from + k - (s.upto[lo] - w.want);
+        w.row[e] = at + i;
+        if (w.copies) {
+          w.copies[0] = w.source;
+          w.copies[1] = at + i;
+        }
+        refs[at + i] = 1;
+        if (k == wanted - 1) s.next = at + i + 1;
+      }
+      ++k;
+    }
+    __syncthreads();
+    scan = s.next < p.pages ? s.next : p.pages;
+    done = done + found < wanted ? done + found : wanted;
+  }
+  __syncthreads();
+  return wanted - done;
+}
+
+// Entries that a row of the table holds, if it is known that it is not what it should be: the first that is no page.
+__device__ int held_entries(const int32_t* row, int most, int pages) {
+  int lo = 0, n = most;
+  while (n > 0) {
+    const int h = n >> 1;
+    if (is_page(row[lo + h], pages)) {
+      lo += h + 1;
+      n -= h + 1;
+    } else {
+      n = h;
+    }
+  }
+  return lo;
+}
+
+__device__ __forceinline__ int need_entries(const ResizeArgs& a, int b) {
+  const int t = a.tokens[b];
+  if (t < 0) return -1;
+  const int64_t n = (int64_t(t) + (1 << a.pool.pshift) - 1) >> a.pool.pshift;
+  return n < a.max_blocks ? int(n) : a.max_blocks;
+}
+
+// Wavefront: a row, whose entries past its need it releases. The workgroup that ends last takes pages for the rows that need
+// them: state[2] counts, and is 0 again when the kernel ends.
+__global__ void __launch_bounds__(kTake) k_pages_resize(ResizeArgs a) {
+  __shared__ TakeLds lds;
+  __shared__ int ended;
+  const int tid = int(threadIdx.x), lane = tid & 63, pages = a.pool.pages;
+  int32_t* refs = a.pool.state + 4;
+  const int b = int(blockIdx.x) * (kTake / 64) + __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int need = b < a.B ? need_entries(a, b) : -1;
+  if (need >= 0) {
+    int32_t* row = a.table + b * a.stride;
+    for (int p = need; p < a.max_blocks; p += 64) {
+      const int e = p + lane < a.max_blocks ? row[p + lane] : -1;
+      const uint64_t hole = __ballot(!is_page(e, pages));
+      const int n = hole ? __ffsll((unsigned long long)hole) - 1 : 64;
+      if (lane < n) {
+        row[p + lane] = -1;
+        if (atomicSub(refs + e, 1) == 1) atomicMin(a.pool.state, e);
+      }
+      if (n < 64) break;
+    }
+  }
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) ended = atomicAdd(a.pool.state + 2, 1);
+  __syncthreads();
+  if (ended != int(gridDim.x) - 1) return;
+  __threadfence();
+  int scan = a.pool.state[0], missing = 0;
+  scan = scan < 0 ? 0 : scan;
+  for (int b0 = 0; b0 < a.B; b0 += kTake) {
+    const int r = b0 + tid;
+    Taking t = {0, 0, nullptr, nullptr, 0};
+    const int n = r < a.B ? need_entries(a, r) : -1;
+    if (n > 0) {
+      t.row = a.table + r * a.stride;
+      if (!is_page(t.row[n - 1], pages)) {   // nearly always it has them, or all but the last, or none
+        t.from = n > 1 && is_page(t.row[n - 2], pages) ? n - 1 : is_page(t.row[0], pages) ? held_entries(t.row, n - 1, pages) : 0;
+        t.want = n - t.from;
+      }
+    }
+    missing += take(a.pool, t, scan, lds);
+  }
+  if (tid == 0) {
+    a.pool.state[0] = scan;
+    a.pool.state[1] = missing;
+    a.pool.state[2] = 0;
+  }
+}
+
+// Whole pages and the partly filled one's entry of a child.
+struct Child {
+  int source, whole, fresh;   // fresh: the page to copy, or -1
+};
+
+__device__ __forceinline__ Child child_of(const ForkArgs& a, int c) {
+  Child k = {a.source[c], 0, -1};
+  if (k.source < 0 || k.source >= a.B) {
+    k.source = -1;
+    return k;
+  }
+  int ctx = a.context[k.source];
+  ctx = ctx < 0 ? 0 : ctx;
+  const int whole = ctx >> a.pool.pshift, part = ctx & ((1 << a.pool.pshift) - 1);
+  const int cap = a.max_blocks < a.child_blocks ? a.max_blocks : a.child_blocks;
+  k.whole = whole < cap ? whole : cap;
+  if (part && whole < cap) {
+    const int e = a.table[k.source * a.stride + whole];
+    k.fresh = is_page(e, a.pool.pages) ? e : -1;
+  }
+  return k;
+}
+
+// Workgroup 0 takes the pages that partly filled ones are copied to; the wavefronts of the others each write a child's row but
+// for that entry. Neither reads what the other writes, but for counts: those that are raised here are of pages in use.
+__global__ void __launch_bounds__(kTake) k_pages_fork(ForkArgs a) {
+  __shared__ TakeLds lds;
+  const int tid = int(threadIdx.x), lane = tid & 63, pages = a.pool.pages;
+  if (blockIdx.x == 0) {
+    int scan = a.pool.state[0], missing = 0;
+    scan = scan < 0 ? 0 : scan;
+    for (int c0 = 0; c0 < a.C; c0 += kTake) {
+      const int c = c0 + tid;
+      Taking t = {0, 0, nullptr, nullptr, 0};
+      if (c < a.C) {
+        const Child k = child_of(a, c);
+        a.copies[2 * c] = a.copies[2 * c + 1] = -1;
+        if (k.fresh >= 0) {
+          t.want = 1;
+          t.from = k.whole;
+          t.row = a.child + c * a.child_stride;
+          t.row[t.from] = -1;
+          t.copies = a.copies + 2 * c;
+          t.source = k.fresh;
+        }
+      }
+      missing += take(a.pool, t, scan, lds);   // its barriers order the -1 above before what it writes
+    }
+    if (tid == 0) {
+      a.pool.state[0] = scan;
+      a.pool.state[1] = missing;
+    }
+    return;
+  }
+  const int c = (int(blockIdx.x) - 1) * (kTake / 64) + __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (c >= a.C) return;
+  const Child k = child_of(a, c);
+  int32_t* row = a.child + c * a.child_stride;
+  const int32_t* from = a.table + (k.source < 0 ? 0 : k.source) * a.stride;
+  int upto = k.whole;
+  for (int p = lane; p - lane < a.child_blocks; p += 64) {
+    int e = p < upto ? from[p] : -1;
+    const uint64_t hole = __ballot(p < upto && !is_page(e, pages));
+    if (hole) {   // the source holds fewer entries than its length says
+      const int first = p - lane + __ffsll((unsigned long long)hole) - 1;
+      upto = first < upto ? first : upto;
+      if (p >= upto) e = -1;
+    }
+    if (p >= a.child_blocks) continue;
+    if (p < upto) atomicAdd(a.pool.state + 4 + e, 1);
+    if (!(k.fresh >= 0 && p == k.whole)) row[p] = e;
+  }
+}
+
+// 16 KB of a page's codes and, with its first piece, the scales of a side.
+__global__ void __launch_bounds__(256) k_kv8_copy_pages(CopyArgs a, int pieces, int64_t items) {
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int64_t c = it / pieces;
+    const int piece = int(it - c * pieces), side = int(blockIdx.y);
+    const int from = a.copies[2 * c], to = a.copies[2 * c + 1];
+    if (!is_page(from, a.from_pages) || !is_page(to, a.to_pages)) continue;
+    const uint8_t* src = a.from[side] + int64_t(from) * a.page_bytes;
+    uint8_t* dst = a.to[side] + int64_t(to) * a.page_bytes;
+    pg_i4 v[4];
+    const int64_t at = int64_t(piece) * 16384 + int64_t(threadIdx.x) * 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (at + 4096 * i < a.page_bytes) v[i] = *reinterpret_cast<const pg_i4*>(src + at + 4096 * i);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (at + 4096 * i < a.page_bytes) *reinterpret_cast<pg_i4*>(dst + at + 4096 * i) = v[i];
+    if (piece == 0)
+      for (int h = int(threadIdx.x); h < a.Hkv; h += 256)
+        a.to_scales[side][int64_t(to) * a.Hkv + h] = a.from_scales[side][int64_t(from) * a.Hkv + h];
+  }
+}
+
+}  // namespace
+
+fluxbin_status launch_pages_resize(const ResizeArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(k_pages_resize, dim3(unsigned(ceil_div(a.B, kTake / 64))), dim3(kTake), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? FLUXBIN_OK : hip_fail(e, "launching the pages' resize");
+}
+
+fluxbin_status launch_pages_fork(const ForkArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(k_pages_fork, dim3(unsigned(1 + ceil_div(a.C, kTake / 64))), dim3(kTake), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? FLUXBIN_OK : hip_fail(e, "launching the pages' fork");
+}
+
+fluxbin_status launch_kv8_copy_pages(const CopyArgs& a, hipStream_t stream) {
+  const int pieces = int(ceil_div(a.page_bytes, 16384));
+  const int64_t items = a.n * pieces, blocks = items < (int64_t(1) << 20) ? items : int64_t(1) << 20;
+  hipLaunchKernelGGL(k_kv8_copy_pages, dim3(unsigned(blocks), 2), dim3(256), 0, stream, a, pieces, items);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? FLUXBIN_OK : hip_fail(e, "launching the pages' copies");
+}
+
+}  // namespace fluxbin

@@ -112,6 +112,8 @@ struct Kv8AttnArgs {
   int32_t chunk_from;               // columns (rows times G) of a sequence from which the prompt chunks' kernel takes it
   int32_t whole;                    // 1: a sequence's column tile and head is not split over workgroups
   float scale2;                     // softmax_scale * log2(e)
+  const uint64_t* masks;            // of trees: [rows][words]
+  int32_t words;
 };
 
 uint64_t kv8_workspace(int32_t D, int cus);

@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libfluxbin (include/fluxbin.h, include/fluxbin_quant.h): argument marshalling only.
+"""Thin ctypes binding of libfluxbin (include/fluxbin.h, fluxbin_quant.h, fluxbin_serve.h): argument marshalling only.
 
 Every step of the hot path runs in the library's HIP kernels; PyTorch only provides device memory and the stream.
 The functions keep the C names. Tensors must be on the current CUDA (HIP) device unless stated otherwise.
@@ -34,6 +34,11 @@ QUANT_EXPORTS = (
     "fluxbin_w4_quantize", "fluxbin_w4_pack_query", "fluxbin_w4_pack", "fluxbin_w4_workspace_query", "fluxbin_w4_gemm",
     "fluxbin_kv8_cache_query", "fluxbin_kv8_append", "fluxbin_kv8_read", "fluxbin_kv8_workspace_query",
     "fluxbin_kv8_attention",
+)
+# Entry points declared in include/fluxbin_serve.h.
+SERVE_EXPORTS = (
+    "fluxbin_qk_rotate", "fluxbin_tree_masks", "fluxbin_kv8_tree_workspace_query", "fluxbin_kv8_tree_attention",
+    "fluxbin_kv8_keep", "fluxbin_pages_resize", "fluxbin_pages_fork", "fluxbin_kv8_copy_pages",
 )
 NOALLOC_SCRATCH_BYTES = 8 << 20
 
@@ -87,6 +92,17 @@ class Kv8Batch(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("sequences", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
                 ("block_table_stride", ctypes.c_int64), ("d_offsets", ctypes.c_void_p), ("d_context", ctypes.c_void_p),
                 ("d_block_table", ctypes.c_void_p)]
+
+
+class Rotary(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("reserved0", ctypes.c_int32), ("eps", ctypes.c_float), ("magnitude", ctypes.c_float),
+                ("d_frequencies", ctypes.c_void_p), ("d_q_weight", ctypes.c_void_p), ("d_k_weight", ctypes.c_void_p)]
+
+
+class PagePoolDesc(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("reserved0", ctypes.c_int32),
+                ("d_state", ctypes.c_void_p)]
 
 
 class Tuning(ctypes.Structure):
@@ -150,7 +166,17 @@ def lib() -> ctypes.CDLL:
         L.fluxbin_kv8_workspace_query.argtypes = [cache_p, i64, i32, i32, ctypes.POINTER(sz)]
         L.fluxbin_kv8_attention.argtypes = [cache_p, batch_p, i32, vp, i64, i64, vp, i64, i64, ctypes.c_float, i32, i32, vp,
                                             sz, vp]
-        for name in EXPORTS + QUANT_EXPORTS:
+        strided = [vp, i64, i64]
+        L.fluxbin_qk_rotate.argtypes = [ctypes.POINTER(Rotary), i64, vp] + 2 * ([i32] + 2 * strided) + [vp]
+        L.fluxbin_tree_masks.argtypes = [i64, i32, vp, vp, vp, i32, vp, vp, vp]
+        L.fluxbin_kv8_tree_workspace_query.argtypes = [cache_p, i64, i32, i32, ctypes.POINTER(sz)]
+        L.fluxbin_kv8_tree_attention.argtypes = [cache_p, batch_p, i32] + 2 * strided + [ctypes.c_float, vp, i32, i32, vp, sz, vp]
+        L.fluxbin_kv8_keep.argtypes = [cache_p, batch_p, vp, vp, vp]
+        pool_p = ctypes.POINTER(PagePoolDesc)
+        L.fluxbin_pages_resize.argtypes = [pool_p, i32, i32, vp, i64, vp, vp]
+        L.fluxbin_pages_fork.argtypes = [pool_p, i32, i32, vp, i64, vp, i32, i32, vp, i64, vp, vp, vp]
+        L.fluxbin_kv8_copy_pages.argtypes = [cache_p, cache_p, i64, vp, vp]
+        for name in EXPORTS + QUANT_EXPORTS + SERVE_EXPORTS:
             if name not in ("fluxbin_status_string", "fluxbin_last_error_message"):
                 getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -660,6 +686,270 @@ def fluxbin_kv8_attention(cache: Kv8Cache, q, offsets, context, block_table, out
     if status:
         _check(status)
     return out
+
+
+# ---- norms and rotation, trees of drafted tokens, pages ----
+
+class RotaryPlan:
+    """What a model's rotation is: its C descriptor and the tensors that it points to."""
+
+    def __init__(self, desc: Rotary, frequencies, q_weight, k_weight):
+        self.desc, self.tensors = desc, (frequencies, q_weight, k_weight)
+        self.head_dim, self.device, self.ref = desc.head_dim, frequencies.device, ctypes.byref(desc)
+        self.index = frequencies.device.index
+        self.use = _Handles()
+
+
+def make_rotary(head_dim: int, frequencies, q_weight=None, k_weight=None, eps: float = 1e-6, magnitude: float = 1.0,
+                interleaved: bool = False) -> RotaryPlan:
+    """Rotation by fp32 frequencies [rotary_dim / 2] (radians per position; empty: norms only) and, where weights are given
+    (fp32 [head_dim]), norms of each head of the queries, of the keys. The tensors are used, not copied."""
+    import torch
+    head_dim = _fits("head_dim", head_dim)
+    _on_device(frequencies.device, q_weight=q_weight, k_weight=k_weight)
+    if frequencies.dim() != 1:
+        raise _invalid(f"frequencies must be [rotary_dim / 2], got {tuple(frequencies.shape)}")
+    _dense("frequencies", frequencies, torch.float32, frequencies.shape)
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _dense(name, w, torch.float32, (head_dim,))
+    desc = Rotary(head_dim, _fits("rotary_dim", 2 * frequencies.shape[0]), 1 if interleaved else 0, 0, eps, magnitude,
+                  frequencies.data_ptr(), _ptr(q_weight), _ptr(k_weight))
+    return RotaryPlan(desc, frequencies, q_weight, k_weight)
+
+
+def _heads(plan, name: str, t, like=None):
+    if t.dim() != 3 or t.dtype is not plan.use.half or t.get_device() != plan.index or t.size(2) != plan.head_dim or \
+            t.stride(2) != 1 or (like is not None and t.shape != like.shape):
+        raise _invalid(f"{name} must be fp16 {list(like.shape) if like is not None else ['rows', 'heads', plan.head_dim]} on "
+                       f"{plan.device} with unit inner stride, got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def fluxbin_qk_rotate(rotary: RotaryPlan, q, k, positions, q_out=None, k_out=None, stream=None):
+    """Norm and rotation of q fp16 [rows, q_heads, head_dim] and k [rows, k_heads, head_dim] (or None), rows and heads at any
+    stride, by positions int32 [rows]. q_out, k_out may be q and k themselves. Returns (q_out, k_out)."""
+    use = rotary.use
+    _heads(rotary, "q", q)
+    rows = q.size(0)
+    if q_out is None:
+        q_out = use.new(stream, *q.shape, dtype=use.half, device=rotary.device)
+    else:
+        _heads(rotary, "q_out", q_out, q)
+    if k is None:
+        k_out, keys = None, (0, None, 0, 0, None, 0, 0)
+    else:
+        _heads(rotary, "k", k)
+        if k.size(0) != rows:
+            raise _invalid(f"q has {rows} rows, k {k.size(0)}")
+        if k_out is None:
+            k_out = use.new(stream, *k.shape, dtype=use.half, device=rotary.device)
+        else:
+            _heads(rotary, "k_out", k_out, k)
+        keys = (k.size(1), k.data_ptr(), k.stride(0), k.stride(1), k_out.data_ptr(), k_out.stride(0), k_out.stride(1))
+    if positions.dtype is not use.int32 or positions.get_device() != rotary.index or positions.dim() != 1 or \
+            positions.size(0) != rows or not positions.is_contiguous():
+        raise _invalid(f"positions must be a contiguous int32 [{rows}] on {rotary.device}")
+    if use.current_device() != rotary.index:
+        raise _invalid(f"operands are on {rotary.device}, which is not the current CUDA (HIP) device")
+    if keys[0] > 0x7FFFFFFF or q.size(1) > 0x7FFFFFFF:
+        raise _invalid("too many heads")
+    status = use.lib.fluxbin_qk_rotate(rotary.ref, rows, positions.data_ptr(), q.size(1), q.data_ptr(), q.stride(0),
+                                       q.stride(1), q_out.data_ptr(), q_out.stride(0), q_out.stride(1), *keys,
+                                       use.stream(stream, rotary.index))
+    if status:
+        _check(status)
+    return q_out, k_out
+
+
+_handles: Optional[_Handles] = None
+
+
+def _use() -> _Handles:
+    global _handles
+    if _handles is None:
+        _handles = _Handles()
+    return _handles
+
+
+def _ints(use, index: int, **arrays) -> None:
+    for name, t in arrays.items():
+        if t.dtype is not use.int32 or t.get_device() != index or t.dim() != 1 or not t.is_contiguous():
+            raise _invalid(f"{name} must be a contiguous int32 vector on the operands' device, got {t.dtype} "
+                           f"{tuple(t.shape)} on {t.device}")
+
+
+def fluxbin_tree_masks(parents, offsets, context, words: int, masks=None, positions=None, stream=None):
+    """Masks int64 [rows, words] (the bits of a node and its ancestors) and positions int32 [rows] of trees, from the index of
+    every node's parent among its sequence's rows (negative: it follows the last cached token). Sequence b has rows
+    offsets[b] .. offsets[b+1] - 1, its newest of context[b] tokens. Up to 64 * words nodes; larger trees are left out."""
+    import torch
+    use, device, index = _use(), parents.device, parents.get_device()
+    if index < 0 or use.current_device() != index:
+        raise _invalid(f"parents are on {device}, which is not the current CUDA (HIP) device")
+    _ints(use, index, parents=parents, offsets=offsets, context=context)
+    rows, B, words = parents.size(0), context.size(0), _fits("words", words)
+    if offsets.size(0) != B + 1 or B > 0x7FFFFFFF:
+        raise _invalid(f"offsets must be [B + 1], context [B], got {offsets.size(0)} and {B}")
+    if words < 1:
+        raise _invalid(f"words = {words} must be >= 1")
+    if masks is None:
+        masks = use.new(stream, rows, words, dtype=torch.int64, device=device)
+    elif masks.dtype is not torch.int64 or masks.get_device() != index or masks.shape != (rows, words) or \
+            not masks.is_contiguous():
+        raise _invalid(f"masks must be a contiguous int64 [{rows}, {words}] on {device}")
+    if positions is None:
+        positions = use.new(stream, rows, dtype=use.int32, device=device)
+    else:
+        _ints(use, index, positions=positions)
+        if positions.size(0) != rows:
+            raise _invalid(f"positions must be [{rows}]")
+    status = use.lib.fluxbin_tree_masks(rows, B, offsets.data_ptr(), context.data_ptr(), parents.data_ptr(), words,
+                                        masks.data_ptr(), positions.data_ptr(), use.stream(stream, index))
+    if status:
+        _check(status)
+    return masks, positions
+
+
+def fluxbin_kv8_tree_workspace_query(cache: Kv8Cache, rows: int, sequences: int, q_heads: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().fluxbin_kv8_tree_workspace_query(cache.ref, _fits("rows", rows, 64), _fits("sequences", sequences),
+                                                  _fits("q_heads", q_heads), ctypes.byref(n)))
+    return n.value
+
+
+def make_kv8_tree_workspace(cache: Kv8Cache, rows: int, sequences: int, q_heads: int, stream=None):
+    """A workspace (torch uint8 tensor, nothing to clear) for tree attention calls of up to that many rows and sequences."""
+    import torch
+    n = fluxbin_kv8_tree_workspace_query(cache, rows, sequences, q_heads)
+    return cache.use.new(stream, max(256, n), dtype=torch.uint8, device=cache.device)
+
+
+def fluxbin_kv8_tree_attention(cache: Kv8Cache, q, masks, offsets, context, block_table, out=None,
+                               scale: Optional[float] = None, window: int = 0, workspace=None, stream=None):
+    """fluxbin_kv8_attention of drafted tokens: a row attends all tokens before its sequence's rows, and of these the ones whose
+    bit is set in its row of masks int64 [rows, words] (as fluxbin_tree_masks makes them); with window > 0 only the last
+    `window` of these. Returns out, fp16 like q; rows of no sequence, or of one with more than 64 * words, are not written."""
+    use, heads = cache.use, q.size(1) if q.dim() == 3 else 0
+    rows = _kv8_rows(cache, "q", q, heads)
+    if out is None:
+        out = use.new(stream, *q.shape, dtype=use.half, device=cache.device)
+    elif rows != _kv8_rows(cache, "out", out, heads):
+        raise _invalid(f"q has {rows} rows, out {out.shape[0]}")
+    if masks.element_size() != 8 or masks.is_floating_point() or masks.is_complex() or masks.get_device() != cache.index or \
+            masks.dim() != 2 or masks.size(0) != rows or not masks.is_contiguous() or masks.size(1) > 0x7FFFFFFF:
+        raise _invalid(f"masks must be a contiguous int64 [{rows}, words] on {cache.device}, got {masks.dtype} "
+                       f"{tuple(masks.shape)} on {masks.device}")
+    b = _kv8_batch(cache, rows, offsets, context, block_table)
+    if workspace is None:
+        workspace = make_kv8_tree_workspace(cache, rows, b.sequences, heads, stream)
+    elif workspace.get_device() != cache.index:
+        raise _invalid(f"workspace is on {workspace.device}, not on {cache.device}")
+    status = use.lib.fluxbin_kv8_tree_attention(cache.ref, ctypes.byref(b), heads, q.data_ptr(), q.stride(0), q.stride(1),
+                                                out.data_ptr(), out.stride(0), out.stride(1),
+                                                cache.head_dim ** -0.5 if scale is None else scale, masks.data_ptr(),
+                                                masks.size(1), max(-1, min(int(window), 0x7FFFFFFF)),
+                                                workspace.data_ptr(), workspace.nbytes, use.stream(stream, cache.index))
+    if status:
+        _check(status)
+    return out
+
+
+def fluxbin_kv8_keep(cache: Kv8Cache, keep, kept, offsets, context, block_table, stream=None) -> None:
+    """Move accepted rows together: of the rows that fluxbin_kv8_append stored with these offsets, context and block_table,
+    sequence b keeps those at indices keep[offsets[b]] < keep[offsets[b] + 1] < ..., kept[b] of them (int32 on the device):
+    the k-th is afterwards at position context[b] - n_b + k. The new lengths, context - n + kept, are the caller's to store."""
+    rows = keep.size(0) if keep.dim() == 1 else -1
+    _ints(cache.use, cache.index, keep=keep, kept=kept)
+    b = _kv8_batch(cache, rows, offsets, context, block_table)
+    if kept.size(0) != b.sequences:
+        raise _invalid(f"kept must be [{b.sequences}], got {kept.size(0)}")
+    status = cache.use.lib.fluxbin_kv8_keep(cache.ref, ctypes.byref(b), keep.data_ptr(), kept.data_ptr(),
+                                            cache.use.stream(stream, cache.index))
+    if status:
+        _check(status)
+
+
+class PagePool:
+    """References of the pages of a pool (torch int32 tensor `state`, all free at first) and its C descriptor. refs: the view
+    of the counts; missing: of the pages that the last call did not find."""
+
+    def __init__(self, state, desc: PagePoolDesc):
+        self.state, self.desc = state, desc
+        self.refs, self.missing = state[4:], state[1:2]
+        self.device, self.ref, self.index = state.device, ctypes.byref(desc), state.device.index
+        self.use = _Handles()
+
+
+def make_page_pool(pages: int, page_size: int, device=None) -> PagePool:
+    import torch
+    pages, page_size = _fits("pages", pages), _fits("page_size", page_size)
+    if pages < 1:
+        raise _invalid(f"pages = {pages} must be >= 1")
+    state = torch.zeros(pages + 4, dtype=torch.int32, device=device or "cuda")
+    return PagePool(state, PagePoolDesc(pages, page_size, 0, state.data_ptr()))
+
+
+def _page_table(pool: PagePool, name: str, t):
+    """(rows, columns, row stride) of a block table."""
+    if t.dtype is not pool.use.int32 or t.get_device() != pool.index or t.dim() != 2 or (t.size(1) > 1 and t.stride(1) != 1) or \
+            t.size(0) > 0x7FFFFFFF or t.size(1) > 0x7FFFFFFF:
+        raise _invalid(f"{name} must be int32 [sequences, blocks] on {pool.device} with unit inner stride, got {t.dtype} "
+                       f"{tuple(t.shape)} on {t.device}")
+    if pool.use.current_device() != pool.index:
+        raise _invalid(f"the pool is on {pool.device}, which is not the current CUDA (HIP) device")
+    return t.size(0), t.size(1), t.size(1) if t.size(0) == 1 else t.stride(0)
+
+
+def fluxbin_pages_resize(pool: PagePool, block_table, tokens, stream=None) -> None:
+    """Give every row of block_table (int32 [B, blocks], changed in place; a new one is filled with -1) the pages of its first
+    tokens[b] tokens (int32 [B]; negative: the row stays): entries past them are released, missing ones taken."""
+    B, blocks, stride = _page_table(pool, "block_table", block_table)
+    _ints(pool.use, pool.index, tokens=tokens)
+    if tokens.size(0) != B:
+        raise _invalid(f"tokens must be [{B}], got {tokens.size(0)}")
+    status = pool.use.lib.fluxbin_pages_resize(pool.ref, B, blocks, block_table.data_ptr(), stride, tokens.data_ptr(),
+                                               pool.use.stream(stream, pool.index))
+    if status:
+        _check(status)
+
+
+def fluxbin_pages_fork(pool: PagePool, block_table, context, source, child_table, copies=None, stream=None):
+    """Make row c of child_table (int32 [C, child_blocks]) that of a copy of sequence source[c] (int32 [C]) of block_table with
+    its context tokens (int32 [B]): full pages are shared, a last partial one is taken anew. Returns copies, int32 [C, 2],
+    (old page, new page) or (-1, -1): what fluxbin_kv8_copy_pages takes, for every layer's cache."""
+    use = pool.use
+    B, blocks, stride = _page_table(pool, "block_table", block_table)
+    C, child_blocks, child_stride = _page_table(pool, "child_table", child_table)
+    _ints(use, pool.index, context=context, source=source)
+    if context.size(0) != B or source.size(0) != C:
+        raise _invalid(f"context must be [{B}], source [{C}], got {context.size(0)} and {source.size(0)}")
+    if copies is None:
+        copies = use.new(stream, C, 2, dtype=use.int32, device=pool.device)
+    elif copies.dtype is not use.int32 or copies.get_device() != pool.index or copies.shape != (C, 2) or \
+            not copies.is_contiguous():
+        raise _invalid(f"copies must be a contiguous int32 [{C}, 2] on {pool.device}")
+    status = use.lib.fluxbin_pages_fork(pool.ref, B, blocks, block_table.data_ptr(), stride, context.data_ptr(), C,
+                                        child_blocks, child_table.data_ptr(), child_stride, source.data_ptr(),
+                                        copies.data_ptr(), use.stream(stream, pool.index))
+    if status:
+        _check(status)
+    return copies
+
+
+def fluxbin_kv8_copy_pages(cache: Kv8Cache, copies, source_cache: Optional[Kv8Cache] = None, stream=None) -> None:
+    """Copy pages copies[i, 0] of source_cache (the same cache by default) to copies[i, 1] of cache (int32 [n, 2]); pairs with a
+    number that is no page are left out."""
+    source = cache if source_cache is None else source_cache
+    if copies.dtype is not cache.use.int32 or copies.get_device() != cache.index or copies.dim() != 2 or \
+            copies.size(1) != 2 or not copies.is_contiguous():
+        raise _invalid(f"copies must be a contiguous int32 [n, 2] on {cache.device}, got {copies.dtype} "
+                       f"{tuple(copies.shape)} on {copies.device}")
+    if source.index != cache.index or cache.use.current_device() != cache.index:
+        raise _invalid(f"the caches are on {cache.device} and {source.device}, which must be the current CUDA (HIP) device")
+    status = cache.use.lib.fluxbin_kv8_copy_pages(cache.ref, source.ref, copies.size(0), copies.data_ptr(),
+                                                  cache.use.stream(stream, cache.index))
+    if status:
+        _check(status)
 
 
 def fluxbin_get_tuning() -> Dict[str, int]:
