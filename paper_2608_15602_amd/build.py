@@ -31,7 +31,7 @@ SOURCES = ["fluxbin_host.cpp", "fluxbin_pack.hip", "fluxbin_gemv.hip", "fluxbin_
            "fluxbin_gemv_rows.hip", "fluxbin_gemm_mfma_rows.hip", "fluxbin_gemm_mx.hip",
            "fluxbin_gemm_prefill.hip", "fluxbin_quant_host.cpp", "fluxbin_w4.hip",
            "fluxbin_kv8.hip", "fluxbin_kv8_attention.hip", "fluxbin_serve_host.cpp", "fluxbin_rotate.hip",
-           "fluxbin_tree.hip", "fluxbin_kv8_keep.hip", "fluxbin_pages.hip"]
+           "fluxbin_tree.hip", "fluxbin_kv8_tree.hip", "fluxbin_kv8_keep.hip", "fluxbin_pages.hip"]
 HOST_SOURCES = ("fluxbin_host.cpp", "fluxbin_quant_host.cpp", "fluxbin_serve_host.cpp")   # what --host-sanitizers instruments
 ARCH = "gfx950"
 

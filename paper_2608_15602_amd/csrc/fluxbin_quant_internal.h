@@ -113,7 +113,7 @@ struct Kv8AttnArgs {
   int32_t whole;                    // 1: a sequence's column tile and head is not split over workgroups
   float scale2;                     // softmax_scale * log2(e)
   const uint64_t* masks;            // of trees: [rows][words]
-  int32_t words;
+  int32_t words, col_shift;         // log2 of the columns of a column tile
 };
 
 uint64_t kv8_workspace(int32_t D, int cus);

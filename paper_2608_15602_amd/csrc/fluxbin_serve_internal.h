@@ -39,6 +39,7 @@ struct MasksArgs {
 
 fluxbin_status launch_tree_masks(const MasksArgs& a, hipStream_t stream);
 
+void launch_kv8_tree_few(Kv8AttnArgs a, int D, int cus, hipStream_t stream);   // col_shift 4
 uint64_t kv8_tree_workspace(int32_t D, int cus);
 fluxbin_status launch_kv8_tree_attention(Kv8AttnArgs a, int D, int cus, hipStream_t stream);
 
