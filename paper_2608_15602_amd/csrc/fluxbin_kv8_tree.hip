@@ -17,10 +17,33 @@ namespace {
 template <int D, int CT>
 constexpr int tree_part() { return 64 * CT * (D + 2); }
 
+// p less one half of `up`, exactly.
+template <int HI>
+__device__ __forceinline__ float rest(kv_h2 up, float p) {
+  float r;
+  if (HI)
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(up), "v"(p));
+  else
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(up), "v"(p));
+  return r;
+}
+
+// A step's matrix instructions, each followed by vector instructions that run beside it.
+template <int MATRIX, int VECTOR>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < MATRIX; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, VECTOR, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 template <int D, int CT>
 __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_tree(Kv8AttnArgs a) {
-  constexpr int kCols = 16 * CT * kWaves, kF = D / 32, kE = D / 16, kU = D / 64;
-  __shared__ __attribute__((aligned(16))) kv_h8 lk[2][4 * kF * 64], lv[2][2 * kE * 64];   // [block][f][lane], [pair][e][lane]
+  constexpr int kCols = 16 * CT * kWaves, kF = D / 32, kE = D / 16, kU = D / 64, kSteps = 2 * kF;
+  __shared__ __attribute__((aligned(16))) kv_h8 lk[2][4 * kF * 64];       // [block of 16 tokens][f][lane]
+  __shared__ __attribute__((aligned(16))) kv_h4 lv[2][2 * kE * 2 * 64];   // [pair of blocks][e][block][lane]
   const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   const int m16 = lane & 15, q4 = lane >> 4;
   Walk<true> walk(a);
@@ -41,19 +64,18 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_tree(Kv8A
     const int t0 = s.t0 + ta, t1 = s.t0 + tb, fresh = s.ctx - s.n;
 
     int lo[CT];
-    const uint64_t* mask[CT];
-    bool has[CT];
+    int rows[CT];   // the columns' rows, -1: there is no such column
     kv_h8 qf[CT][kF];
     int all_lo = 0;
 #pragma unroll
     for (int t = 0; t < CT; ++t) {
       const int col = cb * kCols + (wave * CT + t) * 16 + m16, ci = col / a.G, cg = col - ci * a.G;
-      has[t] = ci < s.n;
-      const int64_t row = s.start + (has[t] ? ci : 0);   // no such column: never stored
-      mask[t] = a.masks + row * a.words;
-      lo[t] = tree_low(a, mask[t], fresh, s.n);
+      const bool has = ci < s.n;
+      const int64_t row = s.start + (has ? ci : 0);   // no such column: never stored
+      rows[t] = has ? s.start + ci : -1;
+      lo[t] = tree_low(a, a.masks + row * a.words, fresh, s.n);
       all_lo = lo[t] > all_lo ? lo[t] : all_lo;
-      const uint16_t* p = a.q + row * a.qts + int64_t(head * a.G + (has[t] ? cg : 0)) * a.qhs;
+      const uint16_t* p = a.q + row * a.qts + int64_t(head * a.G + (has ? cg : 0)) * a.qhs;
 #pragma unroll
       for (int f = 0; f < kF; ++f) __builtin_memcpy(&qf[t][f], p + 32 * f + 8 * q4, 16);
     }
@@ -79,8 +101,9 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_tree(Kv8A
       sum[t] = 0.f;
     }
 
-    // blocks of 16 tokens of 16 tiles, one per lane: pages for the requests; scales; blocks without a page as bits
-    int page = 0;
+    // blocks of 16 tokens of 16 tiles, one per lane: their places in the codes, for the requests; scales; blocks without a page
+    // as bits
+    int64_t place = 0;
     uint64_t holes = 0;
     float kf = 0.f, lvs = 0.f, iv = 0.f;
     auto find = [&](int t) __attribute__((always_inline)) {
@@ -96,104 +119,131 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_tree(Kv8A
       lvs = __builtin_amdgcn_logf(v);
       iv = __builtin_amdgcn_rcpf(v);
     };
+    auto places = [&](int t) __attribute__((always_inline)) {
+      const int p = find(t), tok = t * kTile + 16 * lane;
+      place = kv_page_offset<D>(a.c, p < 0 ? 0 : p, head) + ((tok & ((1 << a.c.pshift) - 1)) >> 4) * 16 * D;
+    };
     auto number = [&](float v, int l) __attribute__((always_inline)) {
       return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l));
     };
     kv_u4 raw[2][kU];   // keys, values
     auto request = [&](int t) __attribute__((always_inline)) {   // this wavefront's block of tile t
-      const int tok = t * kTile + 16 * wave;
-      const int p = __builtin_amdgcn_readlane(page, ((t - t0) & 15) * 4 + wave);
-      const int64_t off = kv_page_offset<D>(a.c, p, head) + int64_t((tok & ((1 << a.c.pshift) - 1)) >> 4) * 16 * D;
+      const int l = ((t - t0) & 15) * 4 + wave;
+      const uint32_t lo32 = uint32_t(__builtin_amdgcn_readlane(int(uint32_t(uint64_t(place))), l));
+      const uint32_t hi32 = uint32_t(__builtin_amdgcn_readlane(int(uint32_t(uint64_t(place) >> 32)), l));
+      const int64_t off = int64_t((uint64_t(hi32) << 32) | lo32);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint8_t* from = h == 1 ? a.c.v : a.c.k;
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int k = 0; k < kU; ++k) raw[h][k] = *reinterpret_cast<const kv_u4*>(from + off + k * 1024 + uint32_t(lane * 16));
+        for (int k = 0; k < kU; ++k)
+          raw[h][k] = *reinterpret_cast<const kv_u4*>((h == 1 ? a.c.v : a.c.k) + off + k * 1024 + uint32_t(lane * 16));
+    };
+    // One of kSteps parts of a tile's decoding: 8 elements of the keys' units, or 4 of two of the values'.
+    auto decode = [&](int buf, int i) __attribute__((always_inline)) {
+      if (i < 2 * kU) {
+        const kv_u4 w = raw[0][i >> 1];
+        lk[buf][(wave * kF + i) * 64 + lane] = i & 1 ? codes8(w.z, w.w) : codes8(w.x, w.y);
+      } else {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const int e = 2 * (i - 2 * kU) + n;
+          lv[buf][(((wave >> 1) * kE + e) * 2 + (wave & 1)) * 64 + lane] = codes4(raw[1][e >> 2][e & 3]);
+        }
       }
     };
-    auto decode = [&](int buf) __attribute__((always_inline)) {
-#pragma unroll
-      for (int k = 0; k < kU; ++k) {
-        lk[buf][(wave * kF + 2 * k) * 64 + lane] = codes8(raw[0][k].x, raw[0][k].y);
-        lk[buf][(wave * kF + 2 * k + 1) * 64 + lane] = codes8(raw[0][k].z, raw[0][k].w);
-      }
-#pragma unroll
-      for (int k = 0; k < kU; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          reinterpret_cast<kv_h4*>(&lv[buf][((wave >> 1) * kE + 4 * k + e) * 64 + lane])[wave & 1] = codes4(raw[1][k][e]);
-    };
-    auto pages = [&](int t) __attribute__((always_inline)) {
-      const int p = find(t);
-      page = p < 0 ? 0 : p;
-    };
-    pages(t0);
+    places(t0);
     look(t0);
     request(t0);
-    decode(0);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) decode(0, i);
     request(t0 + 1 < t1 ? t0 + 1 : t0);
     for (int t = t0; t < t1; ++t) {
-      const int buf = (t - t0) & 1;
+      const int buf = (t - t0) & 1, tok = t * kTile;
       // this tile is decoded, and everyone is done with the other buffer: a barrier for LDS only, requests stay on their way
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-      decode(buf ^ 1);
-      const int tn = t + 2 < t1 ? t + 2 : t1 - 1;
-      if (t + 2 < t1 && ((tn - t0) & 15) == 0) pages(tn);
-      request(tn);
       if (t > t0 && ((t - t0) & 15) == 0) look(t);
-      const int tok = t * kTile;
-      if (!work) continue;
-      float kj[4], lj[4], rj[4];
+      // the next tile's decoding is beside the last products, and its request, for the tile after it, behind them: it has a
+      // tile's time to come
+      auto ahead = [&]() __attribute__((always_inline)) {
+        if (t + 2 < t1 && ((t + 2 - t0) & 15) == 0) places(t + 2);
+        request(t + 2 < t1 ? t + 2 : t1 - 1);
+      };
+      if (!work) {
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) decode(buf ^ 1, i);
+        ahead();
+        continue;
+      }
+      // S: kSteps steps of 2 CT products (half of the tile, 32 elements), operands two steps ahead.
+      kv_h8 kx[3][2];
+      auto keys = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) kx[i % 3][j] = lk[buf][((2 * (i / kF) + j) * kF + i % kF) * 64 + lane];
+      };
+      kv_f4 sc[CT][4];
+      keys(0);
+      keys(1);
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        if (i + 2 < kSteps) keys(i + 2);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            kv_f4& d = sc[c][2 * (i / kF) + j];
+            if (i % kF == 0) d = kv_f4{0.f, 0.f, 0.f, 0.f};
+            d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kx[i % 3][j], qf[c][i % kF], d, 0, 0, 0);
+          }
+      }
+
+      kv_h8 vx[4];
+      auto values = [&](int g) __attribute__((always_inline)) {   // half g / kE of the tile, 16 elements
+        const kv_h4* at = &lv[buf][g * 128 + lane];
+        const kv_h4 x = at[0], y = at[64];
+        vx[g & 3] = kv_h8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+      };
       const uint32_t gone = uint32_t(holes >> (((t - t0) & 15) * 4)) & 15u;
+      float rj[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int l = ((t - t0) & 15) * 4 + j;
-        kj[j] = number(kf, l);
-        lj[j] = number(lvs, l);
+        const float kj = number(kf, l), lj = number(lvs, l);
         rj[j] = number(iv, l);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          const float add = lj - base[c];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[c][j][i] = __builtin_fmaf(sc[c][j][i], kj, add);
+        }
       }
-      kv_f4 sc[CT][4];
+      if (tok < all_lo || tok + kTile > all_hi || gone != 0) {
+        uint64_t in = s.end - tok < 64 ? (uint64_t(1) << (s.end > tok ? s.end - tok : 0)) - 1 : ~uint64_t(0);
 #pragma unroll
-      for (int f = 0; f < kF; ++f)
+        for (int j = 0; j < 4; ++j) in &= gone >> j & 1 ? ~(uint64_t(0xFFFF) << (16 * j)) : ~uint64_t(0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const kv_h8 k = lk[buf][(j * kF + f) * 64 + lane];
-#pragma unroll
-          for (int c = 0; c < CT; ++c) {
-            if (f == 0) sc[c][j] = kv_f4{0.f, 0.f, 0.f, 0.f};
-            sc[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[c][f], sc[c][j], 0, 0, 0);
-          }
-        }
-      kv_h8 ph[CT][2], pl[CT][2];
-#pragma unroll
-      for (int c = 0; c < CT; ++c) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float add = lj[j] - base[c];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sc[c][j][i] = __builtin_fmaf(sc[c][j][i], kj[j], add);
-        }
-        if (tok < all_lo || tok + kTile > all_hi || gone != 0) {
-          const uint64_t seen = has[c] ? tree_bits(mask[c], a.words, tok - fresh, s.n) : 0;
+        for (int c = 0; c < CT; ++c) {
+          uint64_t v = rows[c] < 0 ? 0 : in & tree_bits(a.masks + int64_t(rows[c]) * a.words, a.words, tok - fresh, s.n);
+          if (lo[c] > tok) v = lo[c] - tok < 64 ? v & (~uint64_t(0) << (lo[c] - tok)) : 0;
+          v >>= 4 * q4;   // from this lane's first token on
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int at = tok + 16 * j + 4 * q4 + i;
-              const bool in = at < s.end && at >= lo[c] && !(gone >> j & 1) && (seen >> (16 * j + 4 * q4 + i) & 1);
-              sc[c][j][i] = in ? sc[c][j][i] : -__builtin_inff();
-            }
+            for (int i = 0; i < 4; ++i) sc[c][j][i] = v >> (16 * j + i) & 1 ? sc[c][j][i] : -__builtin_inff();
         }
+      }
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
         float top = -__builtin_inff();
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[c][j][i]);
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
         if (__any(top > limit[c])) {   // scores that are too large for the columns' bases, or their first
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
           // columns with none keep theirs; `by` is finite where there is a score
           const float by = top > limit[c] ? top - kShift : 0.f, r = limit[c] < 0.f ? 0.f : __builtin_amdgcn_exp2f(-by);
           sum[c] *= r;
@@ -206,33 +256,46 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_tree(Kv8A
           base[c] += by;
           limit[c] = top > limit[c] ? kShift + kSlack : limit[c];
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; i += 2) {
-            const float p0 = __builtin_amdgcn_exp2f(sc[c][j][i]), p1 = __builtin_amdgcn_exp2f(sc[c][j][i + 1]);
-            // p before it is rounded: a weight on values of a tiny scale may be lost in p, but not in the sum
-            sum[c] = __builtin_fmaf(p0, rj[j], sum[c]);
-            sum[c] = __builtin_fmaf(p1, rj[j], sum[c]);
-            // the first number cut off (a pair an instruction), the second the rest of it, rounded: 21 bits
-            const kv_h2 up = __builtin_bit_cast(kv_h2, __builtin_amdgcn_cvt_pkrtz(p0, p1));
-            const int at = 4 * (j & 1) + i;
-            ph[c][j >> 1][at] = up.x;
-            ph[c][j >> 1][at + 1] = up.y;
-            pl[c][j >> 1][at] = _Float16(__builtin_fmaf(float(up.x), -1.f, p0));
-            pl[c][j >> 1][at + 1] = _Float16(__builtin_fmaf(float(up.y), -1.f, p1));
-          }
       }
+      // P and O: the weights of one half of the tile are made beside the products of the other.
+      kv_h8 ph[2][CT], pl[2][CT];
+      auto weights = [&](int h, int n) __attribute__((always_inline)) {   // two of a half's 8 CT of a lane
+        const int c = n >> 2, j = (n >> 1) & 1, i = 2 * (n & 1);
+        const float p0 = __builtin_amdgcn_exp2f(sc[c][2 * h + j][i]), p1 = __builtin_amdgcn_exp2f(sc[c][2 * h + j][i + 1]);
+        // p before it is rounded: a weight on values of a tiny scale may be lost in p, but not in the sum
+        sum[c] = __builtin_fmaf(p0, rj[2 * h + j], sum[c]);
+        sum[c] = __builtin_fmaf(p1, rj[2 * h + j], sum[c]);
+        // the first number cut off (a pair an instruction), the second the rest of it, rounded: 21 bits
+        const kv_h2 up = __builtin_bit_cast(kv_h2, __builtin_amdgcn_cvt_pkrtz(p0, p1));
+        ph[h][c][4 * j + i] = up.x;
+        ph[h][c][4 * j + i + 1] = up.y;
+        pl[h][c][4 * j + i] = _Float16(rest<0>(up, p0));
+        pl[h][c][4 * j + i + 1] = _Float16(rest<1>(up, p1));
+      };
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int g = 0; g < 3; ++g) values(g);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int e = 0; e < kE; ++e) {
-          const kv_h8 v = lv[buf][(j * kE + e) * 64 + lane];
+      for (int n = 0; n < 4 * CT; ++n) weights(0, n);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int c = 0; c < CT; ++c) o[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[c][j], o[c][e], 0, 0, 0);
+      for (int g = 0; g < 2 * kE; ++g) {
+        const int h = g / kE, e = g % kE;
+        if (g + 3 < 2 * kE) values(g + 3);
+        if (h == 0) {
 #pragma unroll
-          for (int c = 0; c < CT; ++c) o[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[c][j], o[c][e], 0, 0, 0);
+          for (int n = e * 4 * CT / kE; n < (e + 1) * 4 * CT / kE; ++n) weights(1, n);
+        } else {
+#pragma unroll
+          for (int n = e * kSteps / kE; n < (e + 1) * kSteps / kE; ++n) decode(buf ^ 1, n);
         }
+#pragma unroll
+        for (int c = 0; c < CT; ++c) o[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vx[g & 3], ph[h][c], o[c][e], 0, 0, 0);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) o[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vx[g & 3], pl[h][c], o[c][e], 0, 0, 0);
+        interleave<2 * CT, 4>();
+      }
+      ahead();
     }
     const bool whole = ta == 0 && tb == s.nt;
     float* part = a.part + (int64_t(blockIdx.x) * 2 + (u == u0 ? 0 : 1)) * tree_part<D, CT>();
@@ -266,83 +329,94 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_tree(Kv8A
 }
 
 // Adds the partial results of the items that several workgroups have worked on, in their order. The items are listed first;
-// then a workgroup takes 16 columns and 64 elements of one at a time: 256 threads four elements each, in four slices of the
-// contributions, whose sums are added in LDS.
-constexpr int kJoinWgs = 1024;
+// then a workgroup takes 16 columns and 64 elements of one at a time, its wavefronts each a quarter of the contributions, 4 KB
+// of one at a time; their sums are added in LDS.
+constexpr int kJoinWgs = 1024;   // at most as many records
 
 template <int D, int CT>
-__global__ void __launch_bounds__(1024) k_kv8_tree_join(Kv8AttnArgs a) {
+__global__ void __launch_bounds__(256) k_kv8_tree_join(Kv8AttnArgs a) {
   constexpr int kCols = 16 * CT * kWaves, kE = D / 16, kPieces = CT * kWaves * (kE / 4);
-  __shared__ kv_f4 sums[1024];
-  __shared__ float tops[1024], ls[1024];
-  __shared__ int list[kJoinWgs], found[16];
+  __shared__ kv_f4 sums[4][4][64];
+  __shared__ float tops[4][16], ls[4][16];
+  __shared__ int list[kJoinWgs], found[kJoinWgs / 64];
   const Joint* joints = reinterpret_cast<const Joint*>(a.part + int64_t(a.wgs) * 2 * tree_part<D, CT>());
-  const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int last = tid < a.wgs ? joints[tid].last : 0;
-  const uint64_t mine = __ballot(last > tid && last < a.wgs);
-  if (lane == 0) found[wave] = __popcll((unsigned long long)mine);
-  __syncthreads();
-  int at = 0, count = 0;
-  for (int w = 0; w < 16; ++w) {
-    if (w < wave) at += found[w];
-    count += found[w];
+  const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m16 = lane & 15;
+  uint64_t mine[kJoinWgs / 256];   // of 64 records each
+#pragma unroll
+  for (int i = 0; i < kJoinWgs / 256; ++i) {
+    const int r = i * 256 + tid, last = r < a.wgs ? joints[r].last : 0;
+    mine[i] = __ballot(last > r && last < a.wgs);
+    if (lane == 0) found[i * 4 + wave] = __popcll((unsigned long long)mine[i]);
   }
-  if (mine >> lane & 1) list[at + __popcll((unsigned long long)(mine & ((uint64_t(1) << lane) - 1)))] = tid;
   __syncthreads();
-  const int slice = tid >> 8, e4 = (tid >> 6) & 3;
+  int count = 0;
+#pragma unroll
+  for (int i = 0; i < kJoinWgs / 64; ++i) {
+    if ((i & 3) == wave && (mine[i >> 2] >> lane & 1))
+      list[count + __popcll((unsigned long long)(mine[i >> 2] & ((uint64_t(1) << lane) - 1)))] = i * 64 + lane;
+    count += found[i];
+  }
+  __syncthreads();
   for (int64_t p = blockIdx.x; p < int64_t(count) * kPieces; p += gridDim.x) {
-    const int w0 = list[p / kPieces], piece = int(p % kPieces), tile = piece / (kE / 4), e = (piece % (kE / 4)) * 4 + e4;
+    const int w0 = list[p / kPieces], piece = int(p % kPieces), tile = piece / (kE / 4), e0 = (piece % (kE / 4)) * 4;
     const Joint it = joints[w0];
-    const int n = it.last - w0 + 1, col = tile * 16 + (lane & 15);
+    const int n = it.last - w0 + 1, col = tile * 16 + m16;
     if (it.ct * kCols + tile * 16 >= it.n * a.G) continue;   // no such columns; the same for the whole workgroup
     const float* parts = a.part + int64_t(w0) * 2 * tree_part<D, CT>();
     float top = -__builtin_inff(), l = 0.f;
-    kv_f4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int w = slice; w < n; w += 16) {
-      float m[4], s[4];
-      kv_f4 x[4];
+    kv_f4 v[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {   // contributions past the last repeat it, with no weight
+    for (int e = 0; e < 4; ++e) v[e] = kv_f4{0.f, 0.f, 0.f, 0.f};
+    for (int w = wave; w < n; w += 8) {
+      float m[2], s[2];
+      kv_f4 x[2][4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {   // contributions past the last repeat it, with no weight
         const int wi = w + 4 * i < n ? w + 4 * i : n - 1;
         const float* from = parts + int64_t(2 * wi + (wi == 0 ? it.slot : 0)) * tree_part<D, CT>();
         m[i] = from[kCols * D + col];
         s[i] = from[kCols * D + kCols + col];
-        x[i] = reinterpret_cast<const kv_f4*>(from)[(tile * kE + e) * 64 + lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i][e] = reinterpret_cast<const kv_f4*>(from)[(tile * kE + e0 + e) * 64 + lane];
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 2; ++i) {
         if (w + 4 * i >= n) break;
         const float now = fmaxf(top, m[i]);
         const float r = top == now ? 1.f : __builtin_amdgcn_exp2f(top - now), k = m[i] == now ? 1.f : __builtin_amdgcn_exp2f(m[i] - now);
         l = l * r + s[i] * k;
 #pragma unroll
-        for (int d = 0; d < 4; ++d) v[d] = v[d] * r + x[i][d] * k;
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) v[e][d] = v[e][d] * r + x[i][e][d] * k;
         top = now;
       }
     }
     __syncthreads();   // the piece before
-    tops[tid] = top;
-    ls[tid] = l;
-    sums[tid] = v;
-    __syncthreads();
-    if (slice > 0) continue;
-    float most = top;
+    if (lane < 16) {
+      tops[wave][lane] = top;
+      ls[wave][lane] = l;
+    }
 #pragma unroll
-    for (int i = 1; i < 4; ++i) most = fmaxf(most, tops[tid + 256 * i]);
-    v = kv_f4{0.f, 0.f, 0.f, 0.f};
+    for (int e = 0; e < 4; ++e) sums[wave][e][lane] = v[e];
+    __syncthreads();
+    float most = tops[0][m16];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) most = fmaxf(most, tops[i][m16]);
+    kv_f4 y = {0.f, 0.f, 0.f, 0.f};
     l = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float mi = tops[tid + 256 * i], r = mi == most ? 1.f : __builtin_amdgcn_exp2f(mi - most);
-      const kv_f4 x = sums[tid + 256 * i];
-      l = __builtin_fmaf(ls[tid + 256 * i], r, l);
+      const float mi = tops[i][m16], r = mi == most ? 1.f : __builtin_amdgcn_exp2f(mi - most);
+      const kv_f4 x = sums[i][wave][lane];
+      l = __builtin_fmaf(ls[i][m16], r, l);
 #pragma unroll
-      for (int d = 0; d < 4; ++d) v[d] = __builtin_fmaf(x[d], r, v[d]);
+      for (int d = 0; d < 4; ++d) y[d] = __builtin_fmaf(x[d], r, y[d]);
     }
     Seq q;
     q.start = it.start;
     q.n = it.n;
-    store_out(a, q, it.head, it.ct * kCols + col, 16 * e + 4 * (lane >> 4), v * (l == 0.f ? 0.f : 1.f / l));
+    store_out(a, q, it.head, it.ct * kCols + col, 16 * (e0 + wave) + 4 * (lane >> 4), y * (l == 0.f ? 0.f : 1.f / l));
   }
 }
 
@@ -355,7 +429,7 @@ template <int D, int CT>
 void many_launch(Kv8AttnArgs a, hipStream_t stream) {
   a.col_shift = CT == 1 ? 6 : 7;
   hipLaunchKernelGGL((k_kv8_tree<D, CT>), dim3(unsigned(a.wgs)), dim3(64 * kWaves), 0, stream, a);
-  if (!a.whole) hipLaunchKernelGGL((k_kv8_tree_join<D, CT>), dim3(unsigned(a.wgs)), dim3(1024), 0, stream, a);
+  if (!a.whole) hipLaunchKernelGGL((k_kv8_tree_join<D, CT>), dim3(unsigned(4 * a.wgs)), dim3(256), 0, stream, a);
 }
 
 template <int D>
@@ -366,7 +440,7 @@ void tree_launch(Kv8AttnArgs a, int cus, hipStream_t stream) {
     launch_kv8_tree_few(a, D, cus, stream);
     return;
   }
-  a.wgs = tree_wgs(cus);
+  a.wgs = D == 256 ? tree_wgs(cus) / 2 : tree_wgs(cus);   // as many as run at a time
   a.chunk_from = INT32_MAX;
   a.whole = (int64_t(a.c.max_blocks) << a.c.pshift) <= 15 * kTile;
   if (mean <= 64)

@@ -62,7 +62,7 @@ __device__ __forceinline__ Seq seq_of(const Kv8AttnArgs& a, int b) {
 }
 
 __device__ __forceinline__ int64_t units_of(const Kv8AttnArgs& a, const Seq& s) {
-  return int64_t(s.qt) * a.c.Hkv * (a.whole ? 1 : s.nt);
+  return int64_t(s.qt) * a.c.Hkv * (a.whole ? 1 : s.nt + a.begin);
 }
 
 __device__ __forceinline__ int64_t uniform64(int64_t v) {
