@@ -39,7 +39,7 @@ typedef struct {
 } fluxbin_rotary;
 
 /*
- *   rows         0..2^22, rows * (q_heads + k_heads) * head_dim <= 2^36.   d_positions  int32 [rows].
+ *   rows         0..2^22, rows * (q_heads + k_heads) * head_dim <= 2^35.   d_positions  int32 [rows].
  *   q_heads      1..1024.   k_heads  0..1024 (0: queries only, the keys' arguments are not used).
  *   d_q, d_q_out, d_k, d_k_out  fp16, element (row, head, d) at row * token_stride + head * head_stride + d (strides in
  *                elements, any element alignment). An output may be its own input, at the same strides, and rows may be

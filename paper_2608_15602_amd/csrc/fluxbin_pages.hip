@@ -36,9 +36,7 @@ __device__ __forceinline__ int block_sum(int v, int* red, int& total) {
   return v;
 }
 
-// Takes free pages for the wants of up to kTake rows, in order: `want` entries of this thread's row, from entry `from` of `row`
-// on. scan: the page from which on to look, the same in all threads. Returns how many pages were missing, in all threads.
-// copies, source: where not NULL, (source, page) of this thread's one want.
+// What a thread's row wants: `want` entries from entry `from` on. copies, source: where not NULL, (source, page) of its one want.
 struct Taking {
   int want, from;
   int32_t* row;
@@ -53,25 +51,36 @@ struct TakeLds {
   int next;
 };
 
-__device__ int take(const PoolArgs& p, const Taking& mine, int& scan, TakeLds& s) {
+// Four counts a thread from page `scan` on (the one that its four are a multiple of four from), pages past the last in use.
+__device__ __forceinline__ pg_i4 counts_at(const PoolArgs& p, int scan) {
+  const int32_t* refs = p.state + 4;
+  const int at = (scan & ~3) + 4 * int(threadIdx.x);
+  pg_i4 r = {1, 1, 1, 1};
+  if (at + 3 < p.pages) {
+    r = *reinterpret_cast<const pg_i4*>(refs + at);
+  } else {
+    for (int i = 0; i < 4; ++i)
+      if (at + i < p.pages) r[i] = refs[at + i];
+  }
+  return r;
+}
+
+// Takes free pages for the wants of up to kTake rows, in order. scan: the page from which on to look, the same in all threads, with
+// the counts there. Returns how many pages were missing, in all threads.
+__device__ int take(const PoolArgs& p, const Taking& mine, int& scan, pg_i4& counts, TakeLds& s) {
   const int tid = int(threadIdx.x);
   int wanted;
   const int upto = block_sum(mine.want, s.red, wanted);
+  if (wanted == 0) return 0;
   s.upto[tid] = upto;
   s.who[tid] = mine;
   __syncthreads();
   int32_t* refs = p.state + 4;
   int done = 0;
   while (done < wanted && scan < p.pages) {
-    // four counts a thread; others may raise counts of pages in use meanwhile, not of free ones
+    // others may raise counts of pages in use meanwhile, not of free ones
     const int at = (scan & ~3) + 4 * tid;
-    pg_i4 r = {1, 1, 1, 1};
-    if (at + 3 < p.pages) {
-      r = *reinterpret_cast<const pg_i4*>(refs + at);
-    } else {
-      for (int i = 0; i < 4; ++i)
-        if (at + i < p.pages) r[i] = refs[at + i];
-    }
+    pg_i4 r = counts;
     int free = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -111,22 +120,26 @@ __device__ int take(const PoolArgs& p, const Taking& mine, int& scan, TakeLds& s
     __syncthreads();
     scan = s.next < p.pages ? s.next : p.pages;
     done = done + found < wanted ? done + found : wanted;
+    counts = counts_at(p, scan);   // for the next round or call; what was taken is seen: the barrier is behind it
   }
   __syncthreads();
   return wanted - done;
 }
 
-// Entries that a row of the table holds, if it is known that it is not what it should be: the first that is no page.
+// Entries that a row of the table holds, up to `most`: the first that is no page. Seven places at a time.
 __device__ int held_entries(const int32_t* row, int most, int pages) {
-  int lo = 0, n = most;
+  int lo = 0, n = most;   // it is one of lo .. lo + n
   while (n > 0) {
-    const int h = n >> 1;
-    if (is_page(row[lo + h], pages)) {
-      lo += h + 1;
-      n -= h + 1;
-    } else {
-      n = h;
+    const int step = (n + 7) >> 3;
+    int below = 0;   // places with pages, which come first
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+      const int at = step * i - 1;
+      below += at < n && is_page(row[lo + (at < n ? at : 0)], pages) ? 1 : 0;
     }
+    lo += step * below;
+    n -= step * below;
+    if (below < 7 && n > step - 1) n = step - 1;   // the next place has none
   }
   return lo;
 }
@@ -138,16 +151,34 @@ __device__ __forceinline__ int need_entries(const ResizeArgs& a, int b) {
   return n < a.max_blocks ? int(n) : a.max_blocks;
 }
 
-// Wavefront: a row, whose entries past its need it releases. The workgroup that ends last takes pages for the rows that need
-// them: state[2] counts, and is 0 again when the kernel ends.
+// What row r, of need n, wants.
+__device__ __forceinline__ Taking wants_of(const ResizeArgs& a, int r, int n) {
+  Taking t = {0, 0, nullptr, nullptr, 0};
+  if (n <= 0) return t;
+  t.row = a.table + r * a.stride;
+  // nearly always it has all of them, or all but the last, or none: looked at together
+  const int e1 = t.row[n - 1], e2 = t.row[n > 1 ? n - 2 : 0], e0 = t.row[0];
+  if (is_page(e1, a.pool.pages)) return t;
+  t.from = n > 1 && is_page(e2, a.pool.pages) ? n - 1 : is_page(e0, a.pool.pages) ? held_entries(t.row, n - 1, a.pool.pages) : 0;
+  t.want = n - t.from;
+  return t;
+}
+
+// Wavefront: a row, whose entries past its need it releases. The workgroup that ends last (state[2] counts, and is 0 again when
+// the kernel ends) takes pages for the rows that need them. ONE: there is only one workgroup, which looks at what its rows want
+// while it looks at what they release.
+template <bool ONE>
 __global__ void __launch_bounds__(kTake) k_pages_resize(ResizeArgs a) {
   __shared__ TakeLds lds;
   __shared__ int ended;
   const int tid = int(threadIdx.x), lane = tid & 63, pages = a.pool.pages;
   int32_t* refs = a.pool.state + 4;
-  const int b = int(blockIdx.x) * (kTake / 64) + __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int need = b < a.B ? need_entries(a, b) : -1;
-  if (need >= 0) {
+  Taking mine = {0, 0, nullptr, nullptr, 0};
+  if (ONE && tid < a.B) mine = wants_of(a, tid, need_entries(a, tid));
+  for (int b = int(blockIdx.x) * (kTake / 64) + __builtin_amdgcn_readfirstlane(tid >> 6); b < a.B;
+       b += ONE ? kTake / 64 : a.B) {
+    const int need = need_entries(a, b);
+    if (need < 0) continue;
     int32_t* row = a.table + b * a.stride;
     for (int p = need; p < a.max_blocks; p += 64) {
       const int e = p + lane < a.max_blocks ? row[p + lane] : -1;
@@ -162,29 +193,23 @@ __global__ void __launch_bounds__(kTake) k_pages_resize(ResizeArgs a) {
   }
   __threadfence();
   __syncthreads();
-  if (tid == 0) ended = atomicAdd(a.pool.state + 2, 1);
-  __syncthreads();
-  if (ended != int(gridDim.x) - 1) return;
-  __threadfence();
+  if (!ONE) {
+    if (tid == 0) ended = atomicAdd(a.pool.state + 2, 1);
+    __syncthreads();
+    if (ended != int(gridDim.x) - 1) return;
+    __threadfence();
+  }
   int scan = a.pool.state[0], missing = 0;
   scan = scan < 0 ? 0 : scan;
+  pg_i4 counts = counts_at(a.pool, scan);
   for (int b0 = 0; b0 < a.B; b0 += kTake) {
-    const int r = b0 + tid;
-    Taking t = {0, 0, nullptr, nullptr, 0};
-    const int n = r < a.B ? need_entries(a, r) : -1;
-    if (n > 0) {
-      t.row = a.table + r * a.stride;
-      if (!is_page(t.row[n - 1], pages)) {   // nearly always it has them, or all but the last, or none
-        t.from = n > 1 && is_page(t.row[n - 2], pages) ? n - 1 : is_page(t.row[0], pages) ? held_entries(t.row, n - 1, pages) : 0;
-        t.want = n - t.from;
-      }
-    }
-    missing += take(a.pool, t, scan, lds);
+    if (!ONE) mine = wants_of(a, b0 + tid, b0 + tid < a.B ? need_entries(a, b0 + tid) : -1);
+    missing += take(a.pool, mine, scan, counts, lds);
   }
   if (tid == 0) {
     a.pool.state[0] = scan;
     a.pool.state[1] = missing;
-    a.pool.state[2] = 0;
+    if (!ONE) a.pool.state[2] = 0;
   }
 }
 
@@ -219,6 +244,7 @@ __global__ void __launch_bounds__(kTake) k_pages_fork(ForkArgs a) {
   if (blockIdx.x == 0) {
     int scan = a.pool.state[0], missing = 0;
     scan = scan < 0 ? 0 : scan;
+    pg_i4 counts = counts_at(a.pool, scan);
     for (int c0 = 0; c0 < a.C; c0 += kTake) {
       const int c = c0 + tid;
       Taking t = {0, 0, nullptr, nullptr, 0};
@@ -234,7 +260,7 @@ __global__ void __launch_bounds__(kTake) k_pages_fork(ForkArgs a) {
           t.source = k.fresh;
         }
       }
-      missing += take(a.pool, t, scan, lds);   // its barriers order the -1 above before what it writes
+      missing += take(a.pool, t, scan, counts, lds);   // its barriers order the -1 above before what it writes
     }
     if (tid == 0) {
       a.pool.state[0] = scan;
@@ -288,7 +314,11 @@ __global__ void __launch_bounds__(256) k_kv8_copy_pages(CopyArgs a, int pieces, 
 }  // namespace
 
 fluxbin_status launch_pages_resize(const ResizeArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(k_pages_resize, dim3(unsigned(ceil_div(a.B, kTake / 64))), dim3(kTake), 0, stream, a);
+  // One workgroup for up to two rows a wavefront: without the last workgroup's second look at every row.
+  if (a.B <= kTake / 32)
+    hipLaunchKernelGGL(k_pages_resize<true>, dim3(1), dim3(kTake), 0, stream, a);
+  else
+    hipLaunchKernelGGL(k_pages_resize<false>, dim3(unsigned(ceil_div(a.B, kTake / 64))), dim3(kTake), 0, stream, a);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? FLUXBIN_OK : hip_fail(e, "launching the pages' resize");
 }

@@ -95,8 +95,8 @@ fluxbin_status fluxbin_qk_rotate(const fluxbin_rotary* rotary, int64_t rows, con
     return fail(FLUXBIN_ERR_INVALID_ARG, "rows = %lld out of range [0, 2^22]", (long long)rows);
   if (q_heads < 1 || q_heads > 1024) return fail(FLUXBIN_ERR_INVALID_ARG, "q_heads = %d out of range [1, 1024]", q_heads);
   if (k_heads < 0 || k_heads > 1024) return fail(FLUXBIN_ERR_INVALID_ARG, "k_heads = %d out of range [0, 1024]", k_heads);
-  if (rows * (q_heads + k_heads) * D > (int64_t(1) << 36))   // the kernel's grid has fewer than 2^32 threads
-    return fail(FLUXBIN_ERR_UNSUPPORTED, "rows * heads * head_dim exceeds 2^36");
+  if (rows * (q_heads + k_heads) * D > (int64_t(1) << 35))   // the kernel's grid has fewer than 2^32 threads
+    return fail(FLUXBIN_ERR_UNSUPPORTED, "rows * heads * head_dim exceeds 2^35");
   if (rows > 0 && R > 0 && (!d_positions || misaligned(d_positions, 4)))
     return fail(FLUXBIN_ERR_INVALID_ARG, "positions are NULL or not aligned to their elements");
   Rows q, qo, k{}, ko{};
@@ -117,8 +117,6 @@ fluxbin_status fluxbin_qk_rotate(const fluxbin_rotary* rotary, int64_t rows, con
   if (!clear || any_overlap({qo.range}, {pos, freq, wq, wk}) || any_overlap({ko.range}, {pos, freq, wq, wk}))
     return fail(FLUXBIN_ERR_INVALID_ARG, "the outputs overlap each other or the inputs");
   if (rows == 0) return FLUXBIN_OK;
-  const int cus = device_cu_count();
-  if (cus < 1) return fail(FLUXBIN_ERR_HIP, "reading the device's CU count failed");
   RotateArgs a{};
   a.side[0] = {d_q, d_q_out, rotary->d_q_weight, q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride};
   a.side[1] = {d_k, d_k_out, k_heads > 0 ? rotary->d_k_weight : nullptr, k_token_stride, k_head_stride, k_out_token_stride,
@@ -131,7 +129,7 @@ fluxbin_status fluxbin_qk_rotate(const fluxbin_rotary* rotary, int64_t rows, con
   a.R = R;
   a.eps = rotary->eps;
   a.magnitude = rotary->magnitude;
-  return launch_qk_rotate(a, D, rotary->interleaved, cus, stream);
+  return launch_qk_rotate(a, D, rotary->interleaved, stream);
 }
 
 fluxbin_status fluxbin_tree_masks(int64_t rows, int32_t sequences, const int32_t* d_offsets, const int32_t* d_context,

@@ -25,7 +25,7 @@ struct RotateArgs {
   float eps, magnitude;
 };
 
-fluxbin_status launch_qk_rotate(const RotateArgs& a, int D, int interleaved, int cus, hipStream_t stream);
+fluxbin_status launch_qk_rotate(const RotateArgs& a, int D, int interleaved, hipStream_t stream);
 
 // ---- trees of drafted tokens ----
 struct MasksArgs {

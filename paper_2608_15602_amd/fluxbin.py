@@ -427,7 +427,7 @@ class _Handles:
 
     def __init__(self):
         import torch
-        self.half, self.single, self.int32 = torch.float16, torch.float32, torch.int32
+        self.half, self.single, self.int32, self.int64 = torch.float16, torch.float32, torch.int32, torch.int64
         self.empty = torch.empty
         self.current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -718,44 +718,42 @@ def make_rotary(head_dim: int, frequencies, q_weight=None, k_weight=None, eps: f
     return RotaryPlan(desc, frequencies, q_weight, k_weight)
 
 
-def _heads(plan, name: str, t, like=None):
-    if t.dim() != 3 or t.dtype is not plan.use.half or t.get_device() != plan.index or t.size(2) != plan.head_dim or \
-            t.stride(2) != 1 or (like is not None and t.shape != like.shape):
-        raise _invalid(f"{name} must be fp16 {list(like.shape) if like is not None else ['rows', 'heads', plan.head_dim]} on "
+def _heads(plan, name: str, t, shape=None):
+    """(shape, strides) of fp16 [rows, heads, head_dim] rows: one look at each, a small call's time is that of its Python."""
+    size, stride = t.shape, t.stride()
+    if t.dtype is not plan.use.half or t.get_device() != plan.index or len(size) != 3 or size[2] != plan.head_dim or \
+            stride[2] != 1 or size[1] > 0x7FFFFFFF or (shape is not None and size != shape):
+        raise _invalid(f"{name} must be fp16 {list(shape) if shape is not None else ['rows', 'heads', plan.head_dim]} on "
                        f"{plan.device} with unit inner stride, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return size, stride
 
 
 def fluxbin_qk_rotate(rotary: RotaryPlan, q, k, positions, q_out=None, k_out=None, stream=None):
     """Norm and rotation of q fp16 [rows, q_heads, head_dim] and k [rows, k_heads, head_dim] (or None), rows and heads at any
     stride, by positions int32 [rows]. q_out, k_out may be q and k themselves. Returns (q_out, k_out)."""
-    use = rotary.use
-    _heads(rotary, "q", q)
-    rows = q.size(0)
-    if q_out is None:
-        q_out = use.new(stream, *q.shape, dtype=use.half, device=rotary.device)
-    else:
-        _heads(rotary, "q_out", q_out, q)
-    if k is None:
-        k_out, keys = None, (0, None, 0, 0, None, 0, 0)
-    else:
-        _heads(rotary, "k", k)
-        if k.size(0) != rows:
-            raise _invalid(f"q has {rows} rows, k {k.size(0)}")
-        if k_out is None:
-            k_out = use.new(stream, *k.shape, dtype=use.half, device=rotary.device)
-        else:
-            _heads(rotary, "k_out", k_out, k)
-        keys = (k.size(1), k.data_ptr(), k.stride(0), k.stride(1), k_out.data_ptr(), k_out.stride(0), k_out.stride(1))
-    if positions.dtype is not use.int32 or positions.get_device() != rotary.index or positions.dim() != 1 or \
-            positions.size(0) != rows or not positions.is_contiguous():
-        raise _invalid(f"positions must be a contiguous int32 [{rows}] on {rotary.device}")
-    if use.current_device() != rotary.index:
+    use, index = rotary.use, rotary.index
+    shape, (qt, qh, _) = _heads(rotary, "q", q)
+    rows = shape[0]
+    if use.current_device() != index:
         raise _invalid(f"operands are on {rotary.device}, which is not the current CUDA (HIP) device")
-    if keys[0] > 0x7FFFFFFF or q.size(1) > 0x7FFFFFFF:
-        raise _invalid("too many heads")
-    status = use.lib.fluxbin_qk_rotate(rotary.ref, rows, positions.data_ptr(), q.size(1), q.data_ptr(), q.stride(0),
-                                       q.stride(1), q_out.data_ptr(), q_out.stride(0), q_out.stride(1), *keys,
-                                       use.stream(stream, rotary.index))
+    if q_out is None:
+        q_out = use.new(stream, *shape, dtype=use.half, device=rotary.device)
+    qot, qoh, _ = _heads(rotary, "q_out", q_out, shape)[1]
+    if k is None:
+        k_out, kh, kp, kt, ks, kop, kot, kos = None, 0, None, 0, 0, None, 0, 0
+    else:
+        k_shape, (kt, ks, _) = _heads(rotary, "k", k)
+        if k_shape[0] != rows:
+            raise _invalid(f"q has {rows} rows, k {k_shape[0]}")
+        if k_out is None:
+            k_out = use.new(stream, *k_shape, dtype=use.half, device=rotary.device)
+        kot, kos, _ = _heads(rotary, "k_out", k_out, k_shape)[1]
+        kh, kp, kop = k_shape[1], k.data_ptr(), k_out.data_ptr()
+    if positions.dtype is not use.int32 or positions.get_device() != index or positions.shape != (rows,) or \
+            (rows > 1 and positions.stride(0) != 1):
+        raise _invalid(f"positions must be a contiguous int32 [{rows}] on {rotary.device}")
+    status = use.lib.fluxbin_qk_rotate(rotary.ref, rows, positions.data_ptr(), shape[1], q.data_ptr(), qt, qh, q_out.data_ptr(),
+                                       qot, qoh, kh, kp, kt, ks, kop, kot, kos, use.stream(stream, index))
     if status:
         _check(status)
     return q_out, k_out
@@ -771,38 +769,36 @@ def _use() -> _Handles:
     return _handles
 
 
-def _ints(use, index: int, **arrays) -> None:
-    for name, t in arrays.items():
-        if t.dtype is not use.int32 or t.get_device() != index or t.dim() != 1 or not t.is_contiguous():
-            raise _invalid(f"{name} must be a contiguous int32 vector on the operands' device, got {t.dtype} "
-                           f"{tuple(t.shape)} on {t.device}")
+def _vector(use, index: int, name: str, t, n: int = -1) -> int:
+    """The length of a contiguous int32 vector on device `index`, n if that is given."""
+    size = t.shape
+    if t.dtype is not use.int32 or t.get_device() != index or len(size) != 1 or not t.is_contiguous() or \
+            (n >= 0 and size[0] != n):
+        raise _invalid(f"{name} must be a contiguous int32 vector{f' of {n}' if n >= 0 else ''} on the operands' device, got "
+                       f"{t.dtype} {tuple(size)} on {t.device}")
+    return size[0]
 
 
 def fluxbin_tree_masks(parents, offsets, context, words: int, masks=None, positions=None, stream=None):
     """Masks int64 [rows, words] (the bits of a node and its ancestors) and positions int32 [rows] of trees, from the index of
     every node's parent among its sequence's rows (negative: it follows the last cached token). Sequence b has rows
     offsets[b] .. offsets[b+1] - 1, its newest of context[b] tokens. Up to 64 * words nodes; larger trees are left out."""
-    import torch
-    use, device, index = _use(), parents.device, parents.get_device()
+    use, index, words = _use(), parents.get_device(), _fits("words", words)
     if index < 0 or use.current_device() != index:
-        raise _invalid(f"parents are on {device}, which is not the current CUDA (HIP) device")
-    _ints(use, index, parents=parents, offsets=offsets, context=context)
-    rows, B, words = parents.size(0), context.size(0), _fits("words", words)
-    if offsets.size(0) != B + 1 or B > 0x7FFFFFFF:
-        raise _invalid(f"offsets must be [B + 1], context [B], got {offsets.size(0)} and {B}")
-    if words < 1:
-        raise _invalid(f"words = {words} must be >= 1")
+        raise _invalid(f"parents are on {parents.device}, which is not the current CUDA (HIP) device")
+    rows, B = _vector(use, index, "parents", parents), _vector(use, index, "context", context)
+    _vector(use, index, "offsets", offsets, B + 1)
+    if B > 0x7FFFFFFF or words < 1:
+        raise _invalid(f"{B} sequences, words = {words}: out of range")
     if masks is None:
-        masks = use.new(stream, rows, words, dtype=torch.int64, device=device)
-    elif masks.dtype is not torch.int64 or masks.get_device() != index or masks.shape != (rows, words) or \
+        masks = use.new(stream, rows, words, dtype=use.int64, device=parents.device)
+    elif masks.dtype is not use.int64 or masks.get_device() != index or masks.shape != (rows, words) or \
             not masks.is_contiguous():
-        raise _invalid(f"masks must be a contiguous int64 [{rows}, {words}] on {device}")
+        raise _invalid(f"masks must be a contiguous int64 [{rows}, {words}] on {parents.device}")
     if positions is None:
-        positions = use.new(stream, rows, dtype=use.int32, device=device)
+        positions = use.new(stream, rows, dtype=use.int32, device=parents.device)
     else:
-        _ints(use, index, positions=positions)
-        if positions.size(0) != rows:
-            raise _invalid(f"positions must be [{rows}]")
+        _vector(use, index, "positions", positions, rows)
     status = use.lib.fluxbin_tree_masks(rows, B, offsets.data_ptr(), context.data_ptr(), parents.data_ptr(), words,
                                         masks.data_ptr(), positions.data_ptr(), use.stream(stream, index))
     if status:
@@ -858,11 +854,9 @@ def fluxbin_kv8_keep(cache: Kv8Cache, keep, kept, offsets, context, block_table,
     """Move accepted rows together: of the rows that fluxbin_kv8_append stored with these offsets, context and block_table,
     sequence b keeps those at indices keep[offsets[b]] < keep[offsets[b] + 1] < ..., kept[b] of them (int32 on the device):
     the k-th is afterwards at position context[b] - n_b + k. The new lengths, context - n + kept, are the caller's to store."""
-    rows = keep.size(0) if keep.dim() == 1 else -1
-    _ints(cache.use, cache.index, keep=keep, kept=kept)
+    rows = _vector(cache.use, cache.index, "keep", keep)
     b = _kv8_batch(cache, rows, offsets, context, block_table)
-    if kept.size(0) != b.sequences:
-        raise _invalid(f"kept must be [{b.sequences}], got {kept.size(0)}")
+    _vector(cache.use, cache.index, "kept", kept, b.sequences)
     status = cache.use.lib.fluxbin_kv8_keep(cache.ref, ctypes.byref(b), keep.data_ptr(), kept.data_ptr(),
                                             cache.use.stream(stream, cache.index))
     if status:
@@ -891,22 +885,21 @@ def make_page_pool(pages: int, page_size: int, device=None) -> PagePool:
 
 def _page_table(pool: PagePool, name: str, t):
     """(rows, columns, row stride) of a block table."""
-    if t.dtype is not pool.use.int32 or t.get_device() != pool.index or t.dim() != 2 or (t.size(1) > 1 and t.stride(1) != 1) or \
-            t.size(0) > 0x7FFFFFFF or t.size(1) > 0x7FFFFFFF:
+    size, stride = t.shape, t.stride()
+    if t.dtype is not pool.use.int32 or t.get_device() != pool.index or len(size) != 2 or (size[1] > 1 and stride[1] != 1) or \
+            size[0] > 0x7FFFFFFF or size[1] > 0x7FFFFFFF:
         raise _invalid(f"{name} must be int32 [sequences, blocks] on {pool.device} with unit inner stride, got {t.dtype} "
                        f"{tuple(t.shape)} on {t.device}")
     if pool.use.current_device() != pool.index:
         raise _invalid(f"the pool is on {pool.device}, which is not the current CUDA (HIP) device")
-    return t.size(0), t.size(1), t.size(1) if t.size(0) == 1 else t.stride(0)
+    return size[0], size[1], size[1] if size[0] == 1 else stride[0]
 
 
 def fluxbin_pages_resize(pool: PagePool, block_table, tokens, stream=None) -> None:
     """Give every row of block_table (int32 [B, blocks], changed in place; a new one is filled with -1) the pages of its first
     tokens[b] tokens (int32 [B]; negative: the row stays): entries past them are released, missing ones taken."""
     B, blocks, stride = _page_table(pool, "block_table", block_table)
-    _ints(pool.use, pool.index, tokens=tokens)
-    if tokens.size(0) != B:
-        raise _invalid(f"tokens must be [{B}], got {tokens.size(0)}")
+    _vector(pool.use, pool.index, "tokens", tokens, B)
     status = pool.use.lib.fluxbin_pages_resize(pool.ref, B, blocks, block_table.data_ptr(), stride, tokens.data_ptr(),
                                                pool.use.stream(stream, pool.index))
     if status:
@@ -920,9 +913,8 @@ def fluxbin_pages_fork(pool: PagePool, block_table, context, source, child_table
     use = pool.use
     B, blocks, stride = _page_table(pool, "block_table", block_table)
     C, child_blocks, child_stride = _page_table(pool, "child_table", child_table)
-    _ints(use, pool.index, context=context, source=source)
-    if context.size(0) != B or source.size(0) != C:
-        raise _invalid(f"context must be [{B}], source [{C}], got {context.size(0)} and {source.size(0)}")
+    _vector(use, pool.index, "context", context, B)
+    _vector(use, pool.index, "source", source, C)
     if copies is None:
         copies = use.new(stream, C, 2, dtype=use.int32, device=pool.device)
     elif copies.dtype is not use.int32 or copies.get_device() != pool.index or copies.shape != (C, 2) or \

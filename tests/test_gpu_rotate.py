@@ -86,8 +86,8 @@ def test_norms(fb, norms):
 
 @pytest.mark.parametrize("D,Hq,Hk,inter", [(64, 16, 4, False), (128, 64, 8, False), (128, 3, 2, True), (256, 8, 1, True)])
 def test_many_rows(fb, D, Hq, Hk, inter):
-    """Enough for several pieces a lane, and a ragged end."""
-    T = -(-256 * 8 * 256 // ((Hq + Hk) * (D // 16))) + 5
+    """Outputs past 32 MB, which are streamed."""
+    T = (32 << 20) // (2 * (Hq + Hk) * D) + 5
     log(f"case rotate T={T} D={D}")
     Case(fb, T, Hq, Hk, D, D, inter, seed=5).run()
 
