@@ -48,6 +48,7 @@ struct TakeLds {
   int red[kTake / 64];
   int upto[kTake];
   Taking who[kTake];
+  int list[4 * kTake];   // free pages among those that are looked at
   int next;
 };
 
@@ -88,38 +89,37 @@ __device__ int take(const PoolArgs& p, const Taking& mine, int& scan, pg_i4& cou
       free += r[i] <= 0 ? 1 : 0;
     }
     int found;
-    int k = done + block_sum(free, s.red, found) - free;
+    int k = block_sum(free, s.red, found) - free;
     if (tid == 0) s.next = (scan & ~3) + 4 * kTake;
-    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (r[i] > 0) continue;
-      if (k < wanted) {
-        int lo = 0, n = kTake;   // the first row whose sum is above k
-        while (n > 0) {
-          const int h = n >> 1;
-          if (s.upto[lo + h] <= k) {
-            lo += h + 1;
-            n -= h + 1;
-          } else {
-            n = h;
-          }
+    for (int i = 0; i < 4; ++i)
+      if (r[i] <= 0) s.list[k++] = at + i;
+    __syncthreads();
+    const int n = found < wanted - done ? found : wanted - done;
+    for (int f = tid; f < n; f += kTake) {
+      int lo = 0, rows = kTake;   // the first row whose sum is above that of the page
+      while (rows > 0) {
+        const int h = rows >> 1;
+        if (s.upto[lo + h] <= done + f) {
+          lo += h + 1;
+          rows -= h + 1;
+        } else {
+          rows = h;
         }
-        const Taking& w = s.who[lo];
-        const int e = w.from + k - (s.upto[lo] - w.want);
-        w.row[e] = at + i;
-        if (w.copies) {
-          w.copies[0] = w.source;
-          w.copies[1] = at + i;
-        }
-        refs[at + i] = 1;
-        if (k == wanted - 1) s.next = at + i + 1;
       }
-      ++k;
+      const Taking w = s.who[lo];
+      const int page = s.list[f];
+      w.row[w.from + done + f - (s.upto[lo] - w.want)] = page;
+      if (w.copies) {
+        w.copies[0] = w.source;
+        w.copies[1] = page;
+      }
+      refs[page] = 1;
+      if (done + f == wanted - 1) s.next = page + 1;
     }
     __syncthreads();
     scan = s.next < p.pages ? s.next : p.pages;
-    done = done + found < wanted ? done + found : wanted;
+    done += n;
     counts = counts_at(p, scan);   // for the next round or call; what was taken is seen: the barrier is behind it
   }
   __syncthreads();
@@ -165,16 +165,18 @@ __device__ __forceinline__ Taking wants_of(const ResizeArgs& a, int r, int n) {
 }
 
 // Wavefront: a row, whose entries past its need it releases. The workgroup that ends last (state[2] counts, and is 0 again when
-// the kernel ends) takes pages for the rows that need them. ONE: there is only one workgroup, which looks at what its rows want
-// while it looks at what they release.
+// the kernel ends) takes pages for the rows that need them. Every workgroup looks at what the first kTake rows want while it
+// looks at what its own release (the entries are others): whichever ends last then has it. ONE: there is only one.
 template <bool ONE>
 __global__ void __launch_bounds__(kTake) k_pages_resize(ResizeArgs a) {
   __shared__ TakeLds lds;
-  __shared__ int ended;
+  __shared__ int ended, low;   // the first page that this workgroup freed
   const int tid = int(threadIdx.x), lane = tid & 63, pages = a.pool.pages;
   int32_t* refs = a.pool.state + 4;
   Taking mine = {0, 0, nullptr, nullptr, 0};
-  if (ONE && tid < a.B) mine = wants_of(a, tid, need_entries(a, tid));
+  if (tid == 0) low = INT32_MAX;
+  __syncthreads();
+  if (tid < a.B) mine = wants_of(a, tid, need_entries(a, tid));
   for (int b = int(blockIdx.x) * (kTake / 64) + __builtin_amdgcn_readfirstlane(tid >> 6); b < a.B;
        b += ONE ? kTake / 64 : a.B) {
     const int need = need_entries(a, b);
@@ -186,24 +188,31 @@ __global__ void __launch_bounds__(kTake) k_pages_resize(ResizeArgs a) {
       const int n = hole ? __ffsll((unsigned long long)hole) - 1 : 64;
       if (lane < n) {
         row[p + lane] = -1;
-        if (atomicSub(refs + e, 1) == 1) atomicMin(a.pool.state, e);
+        if (atomicSub(refs + e, 1) == 1) atomicMin(&low, e);
       }
       if (n < 64) break;
     }
   }
-  __threadfence();
   __syncthreads();
-  if (!ONE) {
-    if (tid == 0) ended = atomicAdd(a.pool.state + 2, 1);
-    __syncthreads();
-    if (ended != int(gridDim.x) - 1) return;
-    __threadfence();
+  // What workgroups tell each other are counts and the first free page, by atomics, which have taken place when they have
+  // returned, as all of a workgroup's have before it counts itself; the table's entries that one writes none other reads. So
+  // nothing else has to be written back first (a fence that does took 5 us where the pages' copies were still in the caches).
+  if (tid == 0) {
+    int one = 1;
+    if (low != INT32_MAX) {
+      const int was = atomicMin(a.pool.state, low);
+      asm volatile("" : "+v"(one) : "v"(was));   // it has returned
+    }
+    if (!ONE) ended = atomicAdd(a.pool.state + 2, one);
   }
+  __syncthreads();
+  if (!ONE && ended != int(gridDim.x) - 1) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   int scan = a.pool.state[0], missing = 0;
   scan = scan < 0 ? 0 : scan;
   pg_i4 counts = counts_at(a.pool, scan);
   for (int b0 = 0; b0 < a.B; b0 += kTake) {
-    if (!ONE) mine = wants_of(a, b0 + tid, b0 + tid < a.B ? need_entries(a, b0 + tid) : -1);
+    if (b0 > 0) mine = wants_of(a, b0 + tid, b0 + tid < a.B ? need_entries(a, b0 + tid) : -1);
     missing += take(a.pool, mine, scan, counts, lds);
   }
   if (tid == 0) {
@@ -314,7 +323,7 @@ __global__ void __launch_bounds__(256) k_kv8_copy_pages(CopyArgs a, int pieces, 
 }  // namespace
 
 fluxbin_status launch_pages_resize(const ResizeArgs& a, hipStream_t stream) {
-  // One workgroup for up to two rows a wavefront: without the last workgroup's second look at every row.
+  // One workgroup for up to two rows a wavefront.
   if (a.B <= kTake / 32)
     hipLaunchKernelGGL(k_pages_resize<true>, dim3(1), dim3(kTake), 0, stream, a);
   else
