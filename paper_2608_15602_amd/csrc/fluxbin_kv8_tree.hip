@@ -13,7 +13,8 @@ namespace fluxbin {
 namespace {
 
 // A partial result in the order in which a workgroup holds it: [wavefront][column tile][16 elements][lane] four elements, then
-// the columns' bases and sums. Two for each workgroup (its first and its last item), then a record for each.
+// the columns' bases and sums. Two for each workgroup (its first and its last item), then a record for each, then the records'
+// `last` alone.
 template <int D, int CT>
 constexpr int tree_part() { return 64 * CT * (D + 2); }
 
@@ -325,7 +326,11 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_tree(Kv8A
     u += a.whole ? 1 : tb - ta;
     __syncthreads();   // lds of the next item
   }
-  if (threadIdx.x == 0) reinterpret_cast<Joint*>(a.part + int64_t(a.wgs) * 2 * tree_part<D, CT>())[blockIdx.x] = joint;
+  if (threadIdx.x == 0) {
+    Joint* joints = reinterpret_cast<Joint*>(a.part + int64_t(a.wgs) * 2 * tree_part<D, CT>());
+    joints[blockIdx.x] = joint;
+    reinterpret_cast<int*>(joints + a.wgs)[blockIdx.x] = joint.last;
+  }
 }
 
 // Adds the partial results of the items that several workgroups have worked on, in their order. The items are listed first;
@@ -344,7 +349,7 @@ __global__ void __launch_bounds__(256) k_kv8_tree_join(Kv8AttnArgs a) {
   uint64_t mine[kJoinWgs / 256];   // of 64 records each
 #pragma unroll
   for (int i = 0; i < kJoinWgs / 256; ++i) {
-    const int r = i * 256 + tid, last = r < a.wgs ? joints[r].last : 0;
+    const int r = i * 256 + tid, last = r < a.wgs ? reinterpret_cast<const int*>(joints + a.wgs)[r] : 0;
     mine[i] = __ballot(last > r && last < a.wgs);
     if (lane == 0) found[i * 4 + wave] = __popcll((unsigned long long)mine[i]);
   }
@@ -453,7 +458,7 @@ void tree_launch(Kv8AttnArgs a, int cus, hipStream_t stream) {
 
 uint64_t kv8_tree_workspace(int32_t D, int cus) {
   const uint64_t columns = D == 256 ? 64 : 128;
-  const uint64_t many = round_up256(uint64_t(tree_wgs(cus)) * (2u * columns * (uint64_t(D) + 2) * 4u + sizeof(Joint)));
+  const uint64_t many = round_up256(uint64_t(tree_wgs(cus)) * (2u * columns * (uint64_t(D) + 2) * 4u + sizeof(Joint) + 4u));
   const uint64_t few = kv8_workspace(D, cus);
   return many > few ? many : few;
 }
