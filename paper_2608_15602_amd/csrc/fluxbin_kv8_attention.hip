@@ -629,8 +629,6 @@ static void few_launch(Kv8AttnArgs a, hipStream_t stream) {
 
 void launch_kv8_tree_few(Kv8AttnArgs a, int D, int cus, hipStream_t stream) {
   a.wgs = attention_wgs(cus);
-  a.chunk_from = INT32_MAX;
-  a.whole = (int64_t(a.c.max_blocks) << a.c.pshift) <= 15 * kTile;
   if (D == 64)
     few_launch<64>(a, stream);
   else if (D == 128)

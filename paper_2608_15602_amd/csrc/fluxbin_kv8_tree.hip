@@ -437,18 +437,27 @@ void many_launch(Kv8AttnArgs a, hipStream_t stream) {
   if (!a.whole) hipLaunchKernelGGL((k_kv8_tree_join<D, CT>), dim3(unsigned(4 * a.wgs)), dim3(256), 0, stream, a);
 }
 
+// Which kernel, by columns of a sequence and cached head (their mean: only the device knows each) and by the table's length,
+// which bounds the contexts. Graph-timed, us, 16 columns at a time / 64 a workgroup / 128 a workgroup:
+//   Long tables, heads of 128 over 8: 4 sequences of 8192 tokens, 16, 32, 48, 64, 96, 128 columns 22, 23, 44, 32, 47, 51 / 24, 27,
+//   29, 30, 41, 44 / 31, 31, 37, 37, 40, 43; 2 of 32768 35, 34, 68, 52, 76, 89 / 36, 43, 45, 49, 75, 78 / 46, 45, 57, 56, 60, 65.
+//   Heads of 256, 4 of 4096, 16, 32, 64 columns 33, 35, 41 / 28, 29, 34: 16 at a time decode every code once for one wavefront.
+//   Tables of up to 15 tiles, whose items are not split (a.whole): 16 at a time where those are at most two a CU: 8 sequences of 900
+//   tokens, 64, 128, 256, 512 columns 13, 18, 33, 60 / 24, 25, 26, 37 / 31, 33, 34, 36; 64 of 300, 16, 32, 64, 128 columns 14, 22, 41,
+//   75 / 15, 17, 20, 33 / 19, 20, 25, 30.
 template <int D>
 void tree_launch(Kv8AttnArgs a, int cus, hipStream_t stream) {
-  const int64_t mean = ceil_div(int64_t(a.c.T) * a.G, a.c.B);   // columns of a sequence and cached head
-  if (mean <= 16) {
+  const int64_t mean = ceil_div(int64_t(a.c.T) * a.G, a.c.B);
+  const auto items = [&](int columns) { return int64_t(a.c.B) * ceil_div(mean, columns) * a.c.Hkv; };
+  a.chunk_from = INT32_MAX;
+  a.whole = (int64_t(a.c.max_blocks) << a.c.pshift) <= 15 * kTile;
+  if (a.whole ? items(16) <= 2 * cus : D != 256 && mean <= 32) {
     a.col_shift = 4;
     launch_kv8_tree_few(a, D, cus, stream);
     return;
   }
   a.wgs = D == 256 ? tree_wgs(cus) / 2 : tree_wgs(cus);   // as many as run at a time
-  a.chunk_from = INT32_MAX;
-  a.whole = (int64_t(a.c.max_blocks) << a.c.pshift) <= 15 * kTile;
-  if (mean <= 64)
+  if (mean <= 64 || (a.whole && items(64) <= 2 * cus))
     many_launch<D, 1>(a, stream);
   else
     many_launch<D, most_tiles<D>()>(a, stream);

@@ -149,7 +149,11 @@ def test_left_out(fb):
 @pytest.mark.parametrize("H,G,D,P,new,ctx", [
     (1, 8, 128, 64, [16, 13], [20000, 9000]), (2, 8, 64, 16, [200, 1, 64], [3000, 900, 64]), (8, 8, 128, 64, [64] * 4, [700, 1500, 64, 300]),
     (2, 1, 256, 32, [130], [1700]), (8, 4, 256, 64, [100, 40, 9], [1200, 50, 900]), (40, 1, 128, 128, [128, 33], [400, 2100]),
-    (1, 2, 64, 64, [8] * 300, [40] * 300), (1, 1, 128, 64, [1024], [1500])])
+    (1, 2, 64, 64, [8] * 300, [40] * 300), (1, 1, 128, 64, [1024], [1500]),
+    (2, 8, 128, 64, [4, 3], [5000, 1000]), (2, 8, 64, 16, [1, 5], [3000, 1300]),            # two columns tiles or fewer
+    (2, 8, 128, 64, [6, 7], [3000, 1200]), (2, 8, 64, 32, [5, 8, 0], [2500, 1100, 40]),     # up to 64 columns
+    (8, 8, 128, 16, [5] * 40, [100] * 40), (8, 4, 64, 32, [12] * 39 + [3], [200] * 40),     # short tables, many items
+    (8, 8, 128, 64, [16] * 40, [90] * 40), (8, 16, 64, 16, [9] * 40, [70] * 40), (8, 4, 256, 64, [9] * 40, [120] * 40)])
 def test_large(fb, H, G, D, P, new, ctx):
     """Long histories over many workgroups, many columns, many sequences; the workspace holds NaN where nothing was written."""
     log(f"case tree large H={H} G={G} D={D} new={new[:4]} ctx={ctx[:4]}")
