@@ -165,8 +165,8 @@ __device__ __forceinline__ Taking wants_of(const ResizeArgs& a, int r, int n) {
 }
 
 // Wavefront: a row, whose entries past its need it releases. The workgroup that ends last (state[2] counts, and is 0 again when
-// the kernel ends) takes pages for the rows that need them. Every workgroup looks at what the first kTake rows want while it
-// looks at what its own release (the entries are others): whichever ends last then has it. ONE: there is only one.
+// the kernel ends) takes pages for the rows that need them. Up to kTake rows: every workgroup looks at what they want while it
+// looks at what its own release (the entries are others); whichever ends last then has it. ONE: there is only one.
 template <bool ONE>
 __global__ void __launch_bounds__(kTake) k_pages_resize(ResizeArgs a) {
   __shared__ TakeLds lds;
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(kTake) k_pages_resize(ResizeArgs a) {
   Taking mine = {0, 0, nullptr, nullptr, 0};
   if (tid == 0) low = INT32_MAX;
   __syncthreads();
-  if (tid < a.B) mine = wants_of(a, tid, need_entries(a, tid));
+  if (a.B <= kTake && tid < a.B) mine = wants_of(a, tid, need_entries(a, tid));
   for (int b = int(blockIdx.x) * (kTake / 64) + __builtin_amdgcn_readfirstlane(tid >> 6); b < a.B;
        b += ONE ? kTake / 64 : a.B) {
     const int need = need_entries(a, b);
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(kTake) k_pages_resize(ResizeArgs a) {
   scan = scan < 0 ? 0 : scan;
   pg_i4 counts = counts_at(a.pool, scan);
   for (int b0 = 0; b0 < a.B; b0 += kTake) {
-    if (b0 > 0) mine = wants_of(a, b0 + tid, b0 + tid < a.B ? need_entries(a, b0 + tid) : -1);
+    if (a.B > kTake) mine = wants_of(a, b0 + tid, b0 + tid < a.B ? need_entries(a, b0 + tid) : -1);
     missing += take(a.pool, mine, scan, counts, lds);
   }
   if (tid == 0) {

@@ -78,6 +78,33 @@ def test_resize(fb, pages, P, B, blocks):
     assert (s.plain.refs == 0).all()
 
 
+def test_many_rows_and_pages(fb):
+    """More rows than the workgroup that takes pages has threads, of a pool that it looks through in many rounds, on another
+    stream, and captured."""
+    import torch
+    log("case many rows and pages")
+    s = Pages(fb, 150000, 16, 2500, 70)
+    s.pool.refs[::2] = 1          # pages of others, so that free ones are far apart
+    s.plain.refs[::2] = 1
+    rng = np.random.default_rng(5)
+    s.resize(rng.integers(0, 70 * 16, 2500))
+    tokens, side = s.ints(np.zeros(2500)), torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fb.fluxbin_pages_resize(s.pool, s.t, tokens)
+    for i in range(4):
+        want = rng.integers(-50, 70 * 16, 2500)
+        tokens.copy_(s.ints(want))
+        torch.cuda.synchronize()
+        if i % 2:
+            fb.fluxbin_pages_resize(s.pool, s.t, tokens, stream=side)
+        else:
+            graph.replay()
+        torch.cuda.synchronize()
+        s.plain.resize(s.table, want)
+        s.check()
+
+
 @pytest.mark.parametrize("pages,P,B,C,blocks", [(60, 16, 1, 4, 10), (900, 64, 7, 33, 20), (9000, 32, 30, 1100, 130)])
 def test_fork(fb, pages, P, B, C, blocks):
     """Forks that share and copy, forks of forks, pools that run out, sources that are none, narrower and wider tables."""

@@ -243,6 +243,113 @@ def test_scales_far_apart(fb):
         s.verify([n], 4, q=q * np.float16(20), scale=0.3)
 
 
+@pytest.mark.parametrize("H,G,D,new,ctx", [(2, 4, 64, [5, 9, 3], [300, 20, 77]), (8, 8, 128, [40, 33, 64], [1400, 1200, 1000]),
+                                           (2, 8, 128, [7, 6, 5], [1400, 1200, 1000]), (4, 4, 256, [20, 30, 9], [1100, 1000, 20])])
+def test_queries_not_finite(fb, H, G, D, new, ctx):
+    """NaN and infinities in a query stay in its row and head, with pages missing and masks that leave rows nothing."""
+    log(f"case tree queries not finite H={H} G={G} D={D}")
+    s = Trees(fb, 3, H, D, 32, max(ctx), seed=46)
+    s.append([c - n for c, n in zip(ctx, new)])
+    s.append(new)
+    s.table[1, :] = -1
+    masks = s.masks(new, 1)
+    masks[1] = False
+    q = (s.rng.standard_normal((sum(new), H * G, D))).astype(np.float16)
+    clean = s.verify(new, G, masks=masks, q=q, words=1)
+    bad = q.copy()
+    rows = [0, new[0], sum(new) - 1]
+    bad[rows[0], 0, 3], bad[rows[1], 1, :] = np.nan, np.inf
+    bad[rows[2], H * G - 1, 5] = -np.inf
+    offsets = np.concatenate([[0], np.cumsum(new)])
+    got = fb.fluxbin_kv8_tree_attention(s.cache, s.dev(bad), s.dev(so.packed(masks)), *s.arrays(offsets, s.length)).cpu().double().numpy()
+    assert np.isnan(got[rows[0], 0]).all() and not np.isfinite(got[rows[2], H * G - 1]).any()
+    assert (got[new[0]:new[0] + new[1]] == 0).all()      # no page: nothing is attended, whatever the query
+    for r, h in ((rows[0], 0), (rows[2], H * G - 1)):
+        got[r, h] = clean[r, h]
+    assert np.array_equal(got, clean)
+
+
+@pytest.mark.parametrize("H,G,D,n", [(2, 2, 64, 12), (8, 8, 128, 40), (2, 8, 128, 6), (4, 4, 256, 30)])
+def test_captured(fb, H, G, D, n):
+    """A captured step over lengths and trees that change between replays, on a workspace that an eager call uses too; each
+    replay is what the eager call gives. Then on another stream."""
+    import torch
+    log(f"case tree captured H={H} G={G} D={D} n={n}")
+    s = Trees(fb, 3, H, D, 64, 2000, seed=47)
+    s.append([2000, 2000, 2000])      # every position that a replay may read is stored
+    T, context = 3 * n, s.ints([0, 0, 0])
+    offsets, _, table = s.arrays(np.arange(0, T + 1, n), s.length)
+    q, k, v = (torch.zeros(T, h, D, dtype=torch.float16, device="cuda") for h in (H * G, H, H))
+    masks, ws = torch.zeros(T, 1, dtype=torch.int64, device="cuda"), fb.make_kv8_tree_workspace(s.cache, T, 3, H * G)
+    step = lambda out, stream=None: fb.fluxbin_kv8_tree_attention(s.cache, q, masks, offsets, context, table, out=out, workspace=ws, stream=stream)
+    out = torch.zeros_like(q)
+    step(out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fb.fluxbin_kv8_append(s.cache, k, v, offsets, context, table)
+        step(out)
+    for i in range(5):
+        new = np.array([n] * 3)
+        s.length = np.array([[1500, 200, 900], [64, 1800, 0], [700, 700, 1900], [1, 1, 1], [1300, 0, 30]][i]) + n
+        context.copy_(s.ints(s.length))
+        m = s.masks(new, 1)
+        masks.copy_(s.dev(so.packed(m)))
+        for x in (q, k, v):
+            x.copy_(torch.randn_like(x))
+        graph.replay()
+        torch.cuda.synchronize()
+        captured = out.clone()
+        eager = step(torch.full_like(q, 9.0))
+        torch.cuda.synchronize()
+        assert torch.equal(captured, eager), i
+    side = torch.cuda.Stream()
+    other = torch.full_like(q, 9.0)
+    torch.cuda.synchronize()
+    step(other, side)
+    side.synchronize()
+    assert torch.equal(other, eager)
+
+
+def test_cache_past_32_bits(fb):
+    """Pages whose codes lie past 2^32 bytes: attention of trees with few columns and many, kept rows, copies."""
+    import torch
+    log("case tree large cache")
+    H, D, P, pages = 8, 128, 64, 70000
+    assert pages * H * D * P > 2 ** 32
+    s = Trees(fb, 2, H, D, P, 3 * P, seed=48)
+    s.cache = None
+    s.cache = fb.make_kv8_cache(pages, P, H, D)
+    low = s.table
+    high = np.array([[pages - 1, 0, pages - 2], [pages // 2, pages - 3, 65536]], np.int32)
+    k, v = s.rows(250)
+    offs, lengths, new = [0, 150, 250], np.array([150, 100]), np.array([40, 40])
+    a = s.ints(offs), s.ints(lengths), s.ints(high)
+    fb.fluxbin_kv8_append(s.cache, s.dev(k), s.dev(v), *a)
+    s.plain.append(k, v, offs, lengths, low)
+    rows = np.array([0, 40, 80])
+    s.length = lengths
+    for G in (1, 8):
+        q = s.rng.standard_normal((80, H * G, D)).astype(np.float16)
+        masks = s.masks(new, 1)
+        out = fb.fluxbin_kv8_tree_attention(s.cache, s.dev(q), s.dev(so.packed(masks)), s.ints(rows), a[1], a[2]).cpu().double().numpy()
+        ref, mag, big, peak, _ = s.plain.tree_attention(q, masks, rows, lengths, low, D ** -0.5)
+        assert (np.abs(out - ref) <= qo.attention_bound(ref, mag, big, peak, 150)).all()
+    keep = np.concatenate([np.arange(1, 41, 3), np.zeros(26), np.arange(40)]).astype(np.int32)
+    fb.fluxbin_kv8_keep(s.cache, s.dev(keep), s.ints([14, 40]), s.ints(rows), a[1], a[2])
+    s.plain.keep(keep, [14, 40], rows, lengths, low, 80)
+    lengths = np.array([124, 100])
+    for copy in (False, True):
+        if copy:   # the first sequence's pages to others, and its table with them
+            fb.fluxbin_kv8_copy_pages(s.cache, s.ints([[pages - 1, 1], [0, pages - 5]]))
+            high[0, :2] = 1, pages - 5
+        kt, vt = fb.fluxbin_kv8_read(s.cache, s.ints([0, 124, 224]), s.ints(lengths), s.ints(high), 224)
+        pk, pv, _ = s.plain.read([0, 124, 224], lengths, low, 224)
+        assert np.array_equal(kt.cpu().numpy(), pk) and np.array_equal(vt.cpu().numpy(), pv)
+    s.cache = None
+    torch.cuda.empty_cache()
+
+
 def test_attention_refusals(fb):
     log("case tree refusals")
     s = Trees(fb, 1, 2, 64, 16, 64, seed=19)
