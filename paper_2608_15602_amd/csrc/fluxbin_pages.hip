@@ -156,10 +156,16 @@ __device__ __forceinline__ Taking wants_of(const ResizeArgs& a, int r, int n) {
   Taking t = {0, 0, nullptr, nullptr, 0};
   if (n <= 0) return t;
   t.row = a.table + r * a.stride;
-  // nearly always it has all of them, or all but the last, or none: looked at together
-  const int e1 = t.row[n - 1], e2 = t.row[n > 1 ? n - 2 : 0], e0 = t.row[0];
-  if (is_page(e1, a.pool.pages)) return t;
-  t.from = n > 1 && is_page(e2, a.pool.pages) ? n - 1 : is_page(e0, a.pool.pages) ? held_entries(t.row, n - 1, a.pool.pages) : 0;
+  // Nearly always it has all of them, or all but the last few, or none: looked at together (256 rows of up to 65 pages that grow by
+  // two: 9.4 us; 12.7 with the last two and the first looked at together and the search for the others).
+  int has = 0, e[8];   // the last of them
+#pragma unroll
+  for (int i = 0; i < 8; ++i) e[i] = t.row[n > i ? n - 1 - i : 0];
+  const int e0 = t.row[0];
+#pragma unroll
+  for (int i = 7; i >= 0; --i)
+    if (n > i && is_page(e[i], a.pool.pages)) has = n - i;
+  t.from = has > 0 ? has : n > 8 && is_page(e0, a.pool.pages) ? held_entries(t.row, n - 8, a.pool.pages) : 0;
   t.want = n - t.from;
   return t;
 }
