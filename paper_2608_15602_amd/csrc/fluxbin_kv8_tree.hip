@@ -29,7 +29,8 @@ __device__ __forceinline__ float rest(kv_h2 up, float p) {
   return r;
 }
 
-// A step's matrix instructions, each followed by vector instructions that run beside it.
+// A step's matrix instructions, each followed by vector instructions that run beside it (2 to 6 of them: equal; in any order: 2%
+// slower).
 template <int MATRIX, int VECTOR>
 __device__ __forceinline__ void interleave() {
 #pragma unroll
@@ -40,6 +41,18 @@ __device__ __forceinline__ void interleave() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// Workgroup: a share of the units, as k_kv8_attention's; an item is 64 CT columns of a sequence and cached head. A tile's decoding,
+// scores, weights and output are one barrier apart: the next tile is decoded, from requests sent a tile before, beside the last
+// products, and the weights of the tile's second half beside those of its first. CT = 2 halves the traffic from LDS for a column;
+// its 256 registers allow two workgroups per CU, as do 64 KB of LDS (D = 256: 128 KB, one).
+// Heads of 128, 64 over 8: trees of 48 to 64 rows on 8 sequences of 256 to 8192 tokens 95 us a call, 80 of them here and 13 the join
+// (52 MB of partial results), 428 TFLOP/s by the formula's products, 640 by those done; 13 to 16 rows on 50000 and 65536 tokens
+// 107 us, the join 10, 780 by those done. A wavefront takes 4770 cycles a tile beside another one's, of which its 96 matrix
+// instructions fill 1536 and its 340 others 1900 at their issue; the clock is then at 1.95 GHz. Without the requests the second
+// call takes 20 us less, with requests that hit the cache 3, without the second number of p 14, without exponentials 3.
+// Tried, no faster: products of 32 x 32 with their operands (94, 113), wavefront priorities, uneven shares for a CU's two
+// workgroups, one workgroup per CU, requests two tiles ahead (registers spill: 99 -> 111, 113 -> 123), pages and scales of the
+// next 16 tiles looked up a tile before they are needed (99, 115 against 99, 113 on the same day).
 template <int D, int CT>
 __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_tree(Kv8AttnArgs a) {
   constexpr int kCols = 16 * CT * kWaves, kF = D / 32, kE = D / 16, kU = D / 64, kSteps = 2 * kF;
@@ -335,7 +348,7 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_tree(Kv8A
 
 // Adds the partial results of the items that several workgroups have worked on, in their order. The items are listed first;
 // then a workgroup takes 16 columns and 64 elements of one at a time, its wavefronts each a quarter of the contributions, 4 KB
-// of one at a time; their sums are added in LDS.
+// of one at a time; their sums are added in LDS. 512 workgroups' results, 52 MB, take 13 us: 4 TB/s.
 constexpr int kJoinWgs = 1024;   // at most as many records
 
 template <int D, int CT>

@@ -32,8 +32,8 @@ __device__ __forceinline__ kv_h4 codes4(uint32_t a) {
   return kv_h4{x.x, x.y, y.x, y.y};
 }
 
-// Work of a sequence: column tiles (of 16 columns, for trees what a workgroup takes: row i of the sequence and head g of the group are column i G + g), and
-// token tiles that some row of it attends.
+// Work of a sequence: column tiles (of 16 columns, for trees of what a wavefront or a workgroup takes; row i of the sequence and
+// head g of the group are column i G + g), and token tiles that some row of it attends.
 struct Seq {
   int b, start, n, ctx, end;   // first row, rows, tokens, attendable tokens
   int qt, t0, nt;              // column tiles, first token tile, token tiles
@@ -62,7 +62,7 @@ __device__ __forceinline__ Seq seq_of(const Kv8AttnArgs& a, int b) {
 }
 
 __device__ __forceinline__ int64_t units_of(const Kv8AttnArgs& a, const Seq& s) {
-  return int64_t(s.qt) * a.c.Hkv * (a.whole ? 1 : s.nt + a.begin);
+  return int64_t(s.qt) * a.c.Hkv * (a.whole ? 1 : s.nt);
 }
 
 __device__ __forceinline__ int64_t uniform64(int64_t v) {

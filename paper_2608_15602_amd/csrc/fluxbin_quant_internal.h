@@ -114,7 +114,6 @@ struct Kv8AttnArgs {
   float scale2;                     // softmax_scale * log2(e)
   const uint64_t* masks;            // of trees: [rows][words]
   int32_t words, col_shift;         // log2 of the columns of a column tile
-  int32_t begin;                    // units that an item counts for its beginning
 };
 
 uint64_t kv8_workspace(int32_t D, int cus);

@@ -22,8 +22,9 @@ namespace {
 typedef float rot_f4 __attribute__((ext_vector_type(4)));
 typedef unsigned int rot_u4 __attribute__((ext_vector_type(4), aligned(2)));   // eight elements, at any element's address
 
-// Workgroup: 256 lanes' pieces of the heads of rows in order, of the queries or (blocks from q_blocks on) of the keys. LDS: D floats for each row (16 for each of a head's lanes: four of cosines, sines, as [4][lanes][4], without bank
-// conflicts), then the weight in the same order. STREAM: past the caches' ordinary order.
+// Workgroup: 256 lanes' pieces of the heads of rows in order, of the queries or (blocks from q_blocks on) of the keys. LDS: D
+// floats for each row (16 for each of a head's lanes: four of cosines, sines, as [4][lanes][4], without bank conflicts), then the
+// weight in the same order. STREAM: past the caches' ordinary order.
 template <int D, bool INTER, bool STREAM>
 __global__ void __launch_bounds__(256) k_qk_rotate(RotateArgs a, uint32_t q_blocks) {
   constexpr int L = D / 16;
