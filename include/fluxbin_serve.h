@@ -22,7 +22,7 @@ extern "C" {
  *   y = x * (sum(x^2) / head_dim + eps)^(-1/2) * weight   (only where a weight is given)
  *   then the pair (a, b) of elements i, i < rotary_dim / 2, becomes (a c - b s, a s + b c) with c and s the cosine and sine of
  *   position * frequency[i], both times magnitude; elements from rotary_dim on are not rotated.
- * Held in fp32 and rounded to fp16 once; the angle is an exact product, reduced in 64 bits, so far positions lose nothing.
+ * Held in fp32 and rounded to fp16 once; the angle is formed and reduced in fp64, so that far positions lose nothing.
  *
  *   head_dim       64, 128 or 256.   rotary_dim  a multiple of 16, 0 (norms only) to head_dim.
  *   interleaved    0: a pair is (i, i + rotary_dim / 2), 1: (2 i, 2 i + 1).

@@ -7,9 +7,9 @@
 // head cover it without gaps. Elements from R on go to the lanes behind in pieces of 8 as well. The mean is a sum over the
 // lanes of a head. Cosines and sines are those of a row for all of its heads: a workgroup makes them once, in LDS, while its
 // elements are on their way. An angle is far past 2 pi at far positions (2^20 radians leave an fp32 angle 2^-4): the product is
-// formed in fp64, where it is exact, and brought to half a turn there.
+// formed in fp64, exact up to position 2^29, and brought to half a turn there.
 //
-// Bound by memory: 8192 rows of 64 + 8 heads of 128 from fused rows 54.4 us, 5.55 TB/s (a 1 GiB copy: 5.13 TB/s). Two, four and
+// Bound by memory: 8192 rows of 64 + 8 heads of 128 from fused rows 54 us, 5.55 TB/s (a 1 GiB copy: 5.13 TB/s). Two, four and
 // eight pieces a lane took 61.8, 63.1 and 65.8 us where one took 60.7 (all with ordinary requests); one kernel for both sides that picks
 // strides and weights by lane 75.6. A single row takes 2.9 us under the profiler, of which most is the chain of requests.
 #include "fluxbin_device.h"
