@@ -157,7 +157,7 @@ __device__ __forceinline__ Taking wants_of(const ResizeArgs& a, int r, int n) {
   if (n <= 0) return t;
   t.row = a.table + r * a.stride;
   // Nearly always it has all of them, or all but the last few, or none: looked at together (256 rows of up to 65 pages that grow by
-  // two: 9.4 us; 12.7 with the last two and the first looked at together and the search for the others).
+  // two: 9.4 us; 12.7 with the last two and the first looked at together and a search for the others).
   int has = 0, e[8];   // the last of them
 #pragma unroll
   for (int i = 0; i < 8; ++i) e[i] = t.row[n > i ? n - 1 - i : 0];
@@ -170,10 +170,13 @@ __device__ __forceinline__ Taking wants_of(const ResizeArgs& a, int r, int n) {
   return t;
 }
 
-// Wavefront: a row, whose entries past its need it releases. The workgroup that ends last (state[2] counts, and is 0 again when
-// the kernel ends) takes pages for the rows that need them. Up to kTake rows: every workgroup looks at what they want while it
-// looks at what its own release (the entries are others); whichever ends last then has it. ONE: there is only one.
-// 4 rows 5.1 us released and 4.4 grown by two pages each, 256 rows of up to 65 pages 7.7 and 9.4, with the launch.
+// Wavefront: a row, whose entries past its need it releases. The workgroup that ends last (state[2] counts them, with those that
+// freed pages in its upper half, and is 0 again when the kernel ends) takes pages for the rows that need them. Up to kTake rows:
+// every workgroup looks at what they want and at the free pages while it looks at what its own release. What is wanted is the
+// same for all, for the entries are others; if it is nothing, nobody has to be last. The free pages are as they were unless
+// somebody freed one. ONE: there is only one workgroup.
+// 4 rows 2.7 us released and 2.4 grown by two pages each (5.1 and 4.4 with the free pages looked at afterwards, and by all),
+// 256 rows of up to 65 pages 5.6 and 8.5 (7.7 and 9.4), with the launch.
 template <bool ONE>
 __global__ void __launch_bounds__(kTake) k_pages_resize(ResizeArgs a) {
   __shared__ TakeLds lds;
@@ -181,9 +184,15 @@ __global__ void __launch_bounds__(kTake) k_pages_resize(ResizeArgs a) {
   const int tid = int(threadIdx.x), lane = tid & 63, pages = a.pool.pages;
   int32_t* refs = a.pool.state + 4;
   Taking mine = {0, 0, nullptr, nullptr, 0};
+  int scan = 0, missing = 0;
+  pg_i4 counts = {1, 1, 1, 1};
   if (tid == 0) low = INT32_MAX;
   __syncthreads();
-  if (a.B <= kTake && tid < a.B) mine = wants_of(a, tid, need_entries(a, tid));
+  if (a.B <= kTake) {
+    scan = a.pool.state[0] < 0 ? 0 : a.pool.state[0];
+    counts = counts_at(a.pool, scan);
+    if (tid < a.B) mine = wants_of(a, tid, need_entries(a, tid));
+  }
   for (int b = int(blockIdx.x) * (kTake / 64) + __builtin_amdgcn_readfirstlane(tid >> 6); b < a.B;
        b += ONE ? kTake / 64 : a.B) {
     const int need = need_entries(a, b);
@@ -200,24 +209,30 @@ __global__ void __launch_bounds__(kTake) k_pages_resize(ResizeArgs a) {
       if (n < 64) break;
     }
   }
-  __syncthreads();
+  const bool wanted = __syncthreads_or(a.B > kTake || mine.want > 0), freed = low != INT32_MAX;
+  if (!wanted) {
+    if (tid == 0 && freed) atomicMin(a.pool.state, low);
+    if (tid == 0 && blockIdx.x == 0) a.pool.state[1] = 0;
+    return;
+  }
   // What workgroups tell each other are counts and the first free page, by atomics, which have taken place when they have
   // returned, as all of a workgroup's have before it counts itself; the table's entries that one writes none other reads. So
   // nothing else has to be written back first (a fence that does took 5 us where the pages' copies were still in the caches).
   if (tid == 0) {
-    int one = 1;
-    if (low != INT32_MAX) {
+    int one = freed ? 0x10001 : 1;
+    if (freed) {
       const int was = atomicMin(a.pool.state, low);
       asm volatile("" : "+v"(one) : "v"(was));   // it has returned
     }
-    if (!ONE) ended = atomicAdd(a.pool.state + 2, one);
+    ended = ONE ? 0 : atomicAdd(a.pool.state + 2, one);
   }
   __syncthreads();
-  if (!ONE && ended != int(gridDim.x) - 1) return;
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-  int scan = a.pool.state[0], missing = 0;
-  scan = scan < 0 ? 0 : scan;
-  pg_i4 counts = counts_at(a.pool, scan);
+  if (!ONE && (ended & 0xFFFF) != int(gridDim.x) - 1) return;
+  if (a.B > kTake || freed || ended >> 16) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    scan = a.pool.state[0] < 0 ? 0 : a.pool.state[0];
+    counts = counts_at(a.pool, scan);
+  }
   for (int b0 = 0; b0 < a.B; b0 += kTake) {
     if (a.B > kTake) mine = wants_of(a, b0 + tid, b0 + tid < a.B ? need_entries(a, b0 + tid) : -1);
     missing += take(a.pool, mine, scan, counts, lds);
