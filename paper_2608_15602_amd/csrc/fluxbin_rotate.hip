@@ -2,10 +2,11 @@
 //
 //   y = x * rsqrt(mean(x^2) + eps) * w,   (a, b) -> (a c - b s, a s + b c),   c, s of the angle position * frequency[i].
 //
-// A lane holds 16 elements of a head in two pieces of 8: elements 8 j .. and R / 2 + 8 j .. of the rotated ones (2 x 8 in a row
-// where pairs are neighbours), so that both elements of a pair are in one lane, requests are 16 bytes and the D / 16 lanes of a
-// head cover it without gaps. Elements from R on go to the lanes behind in pieces of 8 as well. The mean is a sum over the
-// lanes of a head. Cosines and sines are those of a row for all of its heads: a workgroup makes them once, in LDS, while its
+// A lane holds 16 elements of a head in two pieces of 8: elements 8 j .. and R / 2 + 8 j .. of the rotated ones, so that both
+// elements of a pair are in one lane, whichever they are, and neighbouring lanes' requests of 16 bytes lie side by side. Elements
+// from R on go to the lanes behind in the same way. (A lane's pieces in a row, for neighbouring pairs and elements from R on: 16384
+// rows of 40 heads of 128 and 256, half of each rotated, 65 and 129 us instead of 62 and 115.) The mean is a sum over the lanes of
+// a head. Cosines and sines are those of a row for all of its heads: a workgroup makes them once, in LDS, while its
 // elements are on their way. An angle is far past 2 pi at far positions (2^20 radians leave an fp32 angle 2^-4): the product is
 // formed in fp64, exact up to position 2^29, and brought to half a turn there.
 //
@@ -39,7 +40,11 @@ __global__ void __launch_bounds__(256) k_qk_rotate(RotateArgs a, uint32_t q_bloc
   const int rows = int((off + units - 1) / hl) + 1;   // from r0 on
   float* weight = lds + rows * D;
   const bool rot = j < a.R / 16;
-  const int c0 = rot ? (INTER ? 16 * j : 8 * j) : 16 * j, c1 = rot && !INTER ? half + 8 * j : c0 + 8;
+  const auto piece = [&](int lane, int second) __attribute__((always_inline)) {   // the first element of a lane's pieces
+    const int rl = a.R / 16;
+    return lane < rl ? 8 * lane + second * half : a.R + 8 * (lane - rl) + second * ((D - a.R) / 2);
+  };
+  const int c0 = piece(j, 0), c1 = piece(j, 1);
 
   const uint32_t at = off + (tid < int(units) ? tid : 0);   // past the end: the first again, not stored
   const uint32_t row = at / hl, head = (at - row * hl) / L;
@@ -54,14 +59,15 @@ __global__ void __launch_bounds__(256) k_qk_rotate(RotateArgs a, uint32_t q_bloc
     const double turns = angle * 0.15915494309189533577;   // 1 / (2 pi)
     float sn, cs;
     sincospif(2.f * float(turns - __builtin_rint(turns)), &sn, &cs);
-    float* to = lds + r * D + (f >> 3) * 4 + (f & 3) + ((f >> 2) & 1) * 4 * L;
+    // the lane's four pairs of its first piece and of its second, or of the first half of its pieces and of the second
+    const int second = INTER ? 2 * f >= half : (f >> 2) & 1, lane = INTER ? (f - second * (half / 2)) >> 2 : f >> 3;
+    float* to = lds + r * D + lane * 4 + (f & 3) + second * 4 * L;
     to[0] = cs * a.magnitude;
     to[8 * L] = sn * a.magnitude;
   }
   if (s.weight && tid < D) {
-    const int piece = tid / (4 * L), lane = (tid / 4) % L, in = (piece & 1) * 4 + (tid & 3);
-    const bool lr = lane < a.R / 16 && !INTER;
-    weight[tid] = s.weight[(piece < 2 ? (lr ? 8 * lane : 16 * lane) : (lr ? half + 8 * lane : 16 * lane + 8)) + in];
+    const int part = tid / (4 * L), lane = (tid / 4) % L;   // four elements of a lane
+    weight[tid] = s.weight[piece(lane, part >> 1) + (part & 1) * 4 + (tid & 3)];
   }
   __syncthreads();
   float y[16];
