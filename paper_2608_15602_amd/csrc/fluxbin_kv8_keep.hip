@@ -22,12 +22,12 @@ __device__ __forceinline__ uint32_t kv_recode4(uint32_t w, float ratio) {
 
 // Workgroup (sequence, head, side): its pages one after another. A page's moved rows go through LDS as rows of codes, brought
 // to the page's new scale, and from there into its 16-byte units; those of earlier tokens are rewritten where the scale grows.
-template <int D>
-__global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
+template <int D, int W>
+__global__ void __launch_bounds__(W) k_kv8_keep(Kv8KeepArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t slab[];   // [rows of a page][D]
-  __shared__ int64_t unit[256];      // of a row: the offset of its block of 16 tokens in the codes, plus its place there
-  __shared__ float ratios[256];
-  __shared__ float red[4];
+  __shared__ int64_t unit[W];      // of a row: the offset of its block of 16 tokens in the codes, plus its place there
+  __shared__ float ratios[W];
+  __shared__ float red[W / 64];
   __shared__ int moved;
   const Kv8Args& c = a.c;
   const int tid = int(threadIdx.x), b = int(blockIdx.x), head = int(blockIdx.y), side = int(blockIdx.z), P = 1 << c.pshift;
@@ -39,12 +39,12 @@ __global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
   // the first row that is not in its place
   if (tid == 0) moved = m;
   __syncthreads();
-  for (int k0 = 0; k0 < m; k0 += 256) {
+  for (int k0 = 0; k0 < m; k0 += W) {
     const int k = k0 + tid;
     if (k < m && a.keep[o0 + k] != k) atomicMin(&moved, k);
     __syncthreads();
     const bool found = moved < m;
-    __syncthreads();   // before the next 256 rows change it
+    __syncthreads();   // before the next rows change it
     if (found) break;
   }
   uint8_t* codes = side ? c.v : c.k;
@@ -79,7 +79,9 @@ __global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
     __syncthreads();   // what the page before left in LDS has been used
     if ((tid & 63) == 0) red[tid >> 6] = s;
     __syncthreads();
-    s = fmaxf(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])), old);
+    s = old;
+#pragma unroll
+    for (int w = 0; w < W / 64; ++w) s = fmaxf(s, red[w]);
     if (tid < count) {
       unit[tid] = u;
       ratios[tid] = s_row < s ? s_row / s : 1.f;
@@ -88,7 +90,7 @@ __global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
     if (tid == 0) *at = s;   // everyone has read the old one: two barriers ago
     __syncthreads();
     if (side == 0) {
-      for (int e = tid; e < count * (D / 16); e += 256) {   // a row's unit: 8 elements from 8 q on, 8 from 32 + 8 q on
+      for (int e = tid; e < count * (D / 16); e += W) {   // a row's unit: 8 elements from 8 q on, 8 from 32 + 8 q on
         const int t = e / (D / 16), blk = e % (D / 16) / 4, q = e % 4;
         const int64_t o = unit[t];
         kv_u4 w = {kKvZero, kKvZero, kKvZero, kKvZero};
@@ -101,7 +103,7 @@ __global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
           *reinterpret_cast<uint32_t*>(&slab[t * D + 64 * blk + 32 * (i >> 1) + 8 * q + 4 * (i & 1)]) = kv_recode4(w[i], ratios[t]);
       }
     } else {
-      for (int e = tid; e < count * (D / 4); e += 256) {   // a unit: elements 16 t + m of four rows
+      for (int e = tid; e < count * (D / 4); e += W) {   // a unit: elements 16 t + m of four rows
         const int t = e / (D / 4), blk = e % (D / 4) / 16, m16 = e % 16;
         const int64_t o = unit[t];
         kv_u4 w = {kKvZero, kKvZero, kKvZero, kKvZero};
@@ -120,7 +122,7 @@ __global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
     }
     __syncthreads();
     uint8_t* to = codes + kv_page_offset<D>(c, page, head);
-    for (int e = (grow != 1.f ? 0 : first >> 4) * D + tid; e < ((last + 15) >> 4) * D; e += 256) {   // D units a block
+    for (int e = (grow != 1.f ? 0 : first >> 4) * D + tid; e < ((last + 15) >> 4) * D; e += W) {   // D units a block
       const int lane = e & 63, blk = (e >> 6) % (D / 64), tb = (e >> 6) / (D / 64), m16 = lane & 15, q = lane >> 4;
       const int t0 = 16 * tb + (side ? 4 * q : m16), t1 = t0 + (side ? 4 : 1);   // the unit's tokens
       const bool fresh = t1 > first && t0 < last;
@@ -151,21 +153,28 @@ __global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
   }
 }
 
+// Threads: at least a page's rows. 128 where there are more workgroups than 256 threads leave room for at a time (8 a CU): 256
+// sequences that keep 8 rows of 64, 8 and 32 heads, 7.9 and 25.2 us, 10.8 and 36.2 with 256; 64 that keep 40, 8 and 32 heads, 9.6 and
+// 18.3, and 8.6 and 20.8 with 256 (64 threads 13.1 and 21.0).
 template <int D>
-void keep_launch(const Kv8KeepArgs& a, hipStream_t stream) {
+void keep_launch(const Kv8KeepArgs& a, int cus, hipStream_t stream) {
   const int P = 1 << a.c.pshift, rows = a.c.T < P ? a.c.T : P;
-  hipLaunchKernelGGL(k_kv8_keep<D>, dim3(unsigned(a.c.B), unsigned(a.c.Hkv), 2), dim3(256), unsigned(rows * D), stream, a);
+  const dim3 grid(unsigned(a.c.B), unsigned(a.c.Hkv), 2);
+  if (P <= 128 && int64_t(a.c.B) * a.c.Hkv * 2 > 8 * cus)
+    hipLaunchKernelGGL((k_kv8_keep<D, 128>), grid, dim3(128), unsigned(rows * D), stream, a);
+  else
+    hipLaunchKernelGGL((k_kv8_keep<D, 256>), grid, dim3(256), unsigned(rows * D), stream, a);
 }
 
 }  // namespace
 
-fluxbin_status launch_kv8_keep(const Kv8KeepArgs& a, int D, hipStream_t stream) {
+fluxbin_status launch_kv8_keep(const Kv8KeepArgs& a, int D, int cus, hipStream_t stream) {
   if (D == 64)
-    keep_launch<64>(a, stream);
+    keep_launch<64>(a, cus, stream);
   else if (D == 128)
-    keep_launch<128>(a, stream);
+    keep_launch<128>(a, cus, stream);
   else
-    keep_launch<256>(a, stream);
+    keep_launch<256>(a, cus, stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? FLUXBIN_OK : hip_fail(e, "launching the cache's moves");
 }

@@ -238,9 +238,11 @@ fluxbin_status fluxbin_kv8_keep(const fluxbin_kv8_cache* cache, const fluxbin_kv
                    offsets_range(*batch), context_range(*batch)}))
     return fail(FLUXBIN_ERR_INVALID_ARG, "the cache overlaps an input");
   if (batch->rows == 0) return FLUXBIN_OK;
+  const int cus = device_cu_count();
+  if (cus < 1) return fail(FLUXBIN_ERR_HIP, "reading the device's CU count failed");
   a.keep = d_keep;
   a.kept = d_kept;
-  return launch_kv8_keep(a, cache->head_dim, stream);
+  return launch_kv8_keep(a, cache->head_dim, cus, stream);
 }
 
 fluxbin_status fluxbin_pages_resize(const fluxbin_page_pool* pool, int32_t sequences, int32_t max_blocks,

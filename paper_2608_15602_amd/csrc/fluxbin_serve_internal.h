@@ -49,7 +49,7 @@ struct Kv8KeepArgs {
   const int32_t* kept;
 };
 
-fluxbin_status launch_kv8_keep(const Kv8KeepArgs& a, int D, hipStream_t stream);
+fluxbin_status launch_kv8_keep(const Kv8KeepArgs& a, int D, int cus, hipStream_t stream);
 
 // ---- pages ----
 struct PoolArgs {

@@ -402,6 +402,19 @@ def test_keep(fb, H, D, P):
     s.check()
 
 
+@pytest.mark.parametrize("P", [16, 128, 256])
+def test_keep_many_sequences(fb, P):
+    """As many workgroups as no longer run at a time."""
+    log(f"case keep of many sequences P={P}")
+    B = 700
+    s = Trees(fb, B, 2, 64, P, P + 60, seed=P)
+    s.append(s.rng.integers(0, P, B))
+    new = s.rng.integers(0, 50, B)
+    s.append(new, 2.0, lambda k, v: (k.__imul__(s.rng.random((len(k), 1, 1)).astype(np.float16) * 4)))
+    _keep(s, new, [np.flatnonzero(s.rng.random(n) < 0.4) for n in new])
+    s.check()
+
+
 def test_keep_special(fb):
     """Rows at positions before 0, missing pages on either side, counts past the rows, zero scales, ranges left out."""
     log("case keep special")
