@@ -347,31 +347,31 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_tree(Kv8A
 }
 
 // Adds the partial results of the items that several workgroups have worked on, in their order. The items are listed first;
-// then a workgroup takes 16 columns and 64 elements of one at a time, its wavefronts each a quarter of the contributions, 4 KB
+// then a workgroup takes 16 columns and 64 elements of one at a time, its wavefronts each a share of the contributions, 4 KB
 // of one at a time; their sums are added in LDS. 512 workgroups' results, 52 MB, take 13 us: 4 TB/s.
 constexpr int kJoinWgs = 1024;   // at most as many records
 
-template <int D, int CT>
-__global__ void __launch_bounds__(256) k_kv8_tree_join(Kv8AttnArgs a) {
+template <int D, int CT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) k_kv8_tree_join(Kv8AttnArgs a) {
   constexpr int kCols = 16 * CT * kWaves, kE = D / 16, kPieces = CT * kWaves * (kE / 4);
-  __shared__ kv_f4 sums[4][4][64];
-  __shared__ float tops[4][16], ls[4][16];
+  __shared__ kv_f4 sums[WAVES][4][64];
+  __shared__ float tops[WAVES][16], ls[WAVES][16];
   __shared__ int list[kJoinWgs], found[kJoinWgs / 64];
   const Joint* joints = reinterpret_cast<const Joint*>(a.part + int64_t(a.wgs) * 2 * tree_part<D, CT>());
   const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m16 = lane & 15;
-  uint64_t mine[kJoinWgs / 256];   // of 64 records each
+  uint64_t mine[kJoinWgs / (64 * WAVES)];   // of 64 records each
 #pragma unroll
-  for (int i = 0; i < kJoinWgs / 256; ++i) {
-    const int r = i * 256 + tid, last = r < a.wgs ? reinterpret_cast<const int*>(joints + a.wgs)[r] : 0;
+  for (int i = 0; i < kJoinWgs / (64 * WAVES); ++i) {
+    const int r = i * 64 * WAVES + tid, last = r < a.wgs ? reinterpret_cast<const int*>(joints + a.wgs)[r] : 0;
     mine[i] = __ballot(last > r && last < a.wgs);
-    if (lane == 0) found[i * 4 + wave] = __popcll((unsigned long long)mine[i]);
+    if (lane == 0) found[i * WAVES + wave] = __popcll((unsigned long long)mine[i]);
   }
   __syncthreads();
   int count = 0;
 #pragma unroll
   for (int i = 0; i < kJoinWgs / 64; ++i) {
-    if ((i & 3) == wave && (mine[i >> 2] >> lane & 1))
-      list[count + __popcll((unsigned long long)(mine[i >> 2] & ((uint64_t(1) << lane) - 1)))] = i * 64 + lane;
+    if (i % WAVES == wave && (mine[i / WAVES] >> lane & 1))
+      list[count + __popcll((unsigned long long)(mine[i / WAVES] & ((uint64_t(1) << lane) - 1)))] = i * 64 + lane;
     count += found[i];
   }
   __syncthreads();
@@ -385,12 +385,12 @@ __global__ void __launch_bounds__(256) k_kv8_tree_join(Kv8AttnArgs a) {
     kv_f4 v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = kv_f4{0.f, 0.f, 0.f, 0.f};
-    for (int w = wave; w < n; w += 8) {
+    for (int w = wave; w < n; w += 2 * WAVES) {
       float m[2], s[2];
       kv_f4 x[2][4];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {   // contributions past the last repeat it, with no weight
-        const int wi = w + 4 * i < n ? w + 4 * i : n - 1;
+        const int wi = w + WAVES * i < n ? w + WAVES * i : n - 1;
         const float* from = parts + int64_t(2 * wi + (wi == 0 ? it.slot : 0)) * tree_part<D, CT>();
         m[i] = from[kCols * D + col];
         s[i] = from[kCols * D + kCols + col];
@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(256) k_kv8_tree_join(Kv8AttnArgs a) {
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        if (w + 4 * i >= n) break;
+        if (w + WAVES * i >= n) break;
         const float now = fmaxf(top, m[i]);
         const float r = top == now ? 1.f : __builtin_amdgcn_exp2f(top - now), k = m[i] == now ? 1.f : __builtin_amdgcn_exp2f(m[i] - now);
         l = l * r + s[i] * k;
@@ -418,13 +418,14 @@ __global__ void __launch_bounds__(256) k_kv8_tree_join(Kv8AttnArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) sums[wave][e][lane] = v[e];
     __syncthreads();
+    if (wave >= 4) continue;   // the others have a quarter of the elements each
     float most = tops[0][m16];
 #pragma unroll
-    for (int i = 1; i < 4; ++i) most = fmaxf(most, tops[i][m16]);
+    for (int i = 1; i < WAVES; ++i) most = fmaxf(most, tops[i][m16]);
     kv_f4 y = {0.f, 0.f, 0.f, 0.f};
     l = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < WAVES; ++i) {
       const float mi = tops[i][m16], r = mi == most ? 1.f : __builtin_amdgcn_exp2f(mi - most);
       const kv_f4 x = sums[i][wave][lane];
       l = __builtin_fmaf(ls[i][m16], r, l);
@@ -444,17 +445,25 @@ template <int D>
 constexpr int most_tiles() { return D == 256 ? 1 : 2; }   // column tiles of a wavefront
 
 template <int D, int CT>
-void many_launch(Kv8AttnArgs a, hipStream_t stream) {
+void many_launch(Kv8AttnArgs a, int64_t items, hipStream_t stream) {
   a.col_shift = CT == 1 ? 6 : 7;
   hipLaunchKernelGGL((k_kv8_tree<D, CT>), dim3(unsigned(a.wgs)), dim3(64 * kWaves), 0, stream, a);
-  if (!a.whole) hipLaunchKernelGGL((k_kv8_tree_join<D, CT>), dim3(unsigned(4 * a.wgs)), dim3(256), 0, stream, a);
+  if (a.whole) return;
+  // Contributions to an item, as far as the host can tell. Many: 16 wavefronts to a piece. One sequence of 100000 tokens and 16 heads
+  // over one, 64, 128 and 256 columns, 38, 44 and 45 us, 62, 68 and 59 with 4; 16 of 2000, 256 columns, 8 contributions, 29 and 26.
+  const int64_t tiles = ((int64_t(a.c.max_blocks) << a.c.pshift) + kTile - 1) / kTile, each = a.wgs / items;
+  if ((each < tiles / kWaves ? each : tiles / kWaves) >= 32)
+    hipLaunchKernelGGL((k_kv8_tree_join<D, CT, 16>), dim3(unsigned(a.wgs)), dim3(1024), 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_kv8_tree_join<D, CT, 4>), dim3(unsigned(4 * a.wgs)), dim3(256), 0, stream, a);
 }
 
 // Which kernel, by columns of a sequence and cached head (their mean: only the device knows each) and by the table's length,
 // which bounds the contexts. Graph-timed, us, 16 columns at a time / 64 a workgroup / 128 a workgroup:
 //   Long tables, heads of 128 over 8: 4 sequences of 8192 tokens, 16, 32, 48, 64, 96, 128 columns 22, 23, 44, 32, 47, 51 / 24, 27,
 //   29, 30, 41, 44 / 31, 31, 37, 37, 40, 43; 2 of 32768 35, 34, 68, 52, 76, 89 / 36, 43, 45, 49, 75, 78 / 46, 45, 57, 56, 60, 65.
-//   Heads of 256, 4 of 4096, 16, 32, 64 columns 33, 35, 41 / 28, 29, 34: 16 at a time decode every code once for one wavefront.
+//   Heads of 256, 4 of 4096, 32, 64 columns 35, 41 / 29, 34: 16 at a time decode every code once for one wavefront. 16 columns 33 /
+//   28; 64 of 4000 176 / 250, 256 of 500 161 / 174; 4 columns 169 / 262 and 135 / 173: codes past the caches' ordinary order.
 //   Tables of up to 15 tiles, whose items are not split (a.whole): 16 at a time where those are at most two a CU: 8 sequences of 900
 //   tokens, 64, 128, 256, 512 columns 13, 18, 33, 60 / 24, 25, 26, 37 / 31, 33, 34, 36; 64 of 300, 16, 32, 64, 128 columns 14, 22, 41,
 //   75 / 15, 17, 20, 33 / 19, 20, 25, 30.
@@ -464,16 +473,16 @@ void tree_launch(Kv8AttnArgs a, int cus, hipStream_t stream) {
   const auto items = [&](int columns) { return int64_t(a.c.B) * ceil_div(mean, columns) * a.c.Hkv; };
   a.chunk_from = INT32_MAX;
   a.whole = (int64_t(a.c.max_blocks) << a.c.pshift) <= 15 * kTile;
-  if (a.whole ? items(16) <= 2 * cus : D != 256 && mean <= 32) {
+  if (mean <= 16 || (a.whole ? items(16) <= 2 * cus : D != 256 && mean <= 32)) {
     a.col_shift = 4;
     launch_kv8_tree_few(a, D, cus, stream);
     return;
   }
   a.wgs = D == 256 ? tree_wgs(cus) / 2 : tree_wgs(cus);   // as many as run at a time
   if (mean <= 64 || (a.whole && items(64) <= 2 * cus))
-    many_launch<D, 1>(a, stream);
+    many_launch<D, 1>(a, items(64), stream);
   else
-    many_launch<D, most_tiles<D>()>(a, stream);
+    many_launch<D, most_tiles<D>()>(a, items(64 * most_tiles<D>()), stream);
 }
 
 }  // namespace
