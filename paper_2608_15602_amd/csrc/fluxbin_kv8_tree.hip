@@ -45,9 +45,9 @@ __device__ __forceinline__ void interleave() {
 // scores, weights and output are one barrier apart: the next tile is decoded, from requests sent a tile before, beside the last
 // products, and the weights of the tile's second half beside those of its first. CT = 2 halves the traffic from LDS for a column;
 // its 256 registers allow two workgroups per CU, as do 64 KB of LDS (D = 256: 128 KB, one).
-// Heads of 128, 64 over 8: trees of 48 to 64 rows on 8 sequences of 256 to 8192 tokens 95 us a call, 80 of them here and 13 the join
+// Heads of 128, 64 over 8: trees of 48 to 64 rows on 8 sequences of 256 to 8192 tokens 94 us a call, 80 of them here and 13 the join
 // (52 MB of partial results), 428 TFLOP/s by the formula's products, 640 by those done; 13 to 16 rows on 50000 and 65536 tokens
-// 107 us, the join 10, 780 by those done. A wavefront takes 4770 cycles a tile beside another one's, of which its 96 matrix
+// 105 us, the join 10, 790 by those done. A wavefront takes 4770 cycles a tile beside another one's, of which its 96 matrix
 // instructions fill 1536 and its 340 others 1900 at their issue; the clock is then at 1.95 GHz. Without the requests the second
 // call takes 20 us less, with requests that hit the cache 3, without the second number of p 14, without exponentials 3.
 // Tried, no faster: products of 32 x 32 with their operands (94, 113), wavefront priorities, uneven shares for a CU's two
@@ -445,44 +445,56 @@ template <int D>
 constexpr int most_tiles() { return D == 256 ? 1 : 2; }   // column tiles of a wavefront
 
 template <int D, int CT>
-void many_launch(Kv8AttnArgs a, int64_t items, hipStream_t stream) {
+void many_launch(Kv8AttnArgs a, int64_t items, int64_t tiles, hipStream_t stream) {
   a.col_shift = CT == 1 ? 6 : 7;
   hipLaunchKernelGGL((k_kv8_tree<D, CT>), dim3(unsigned(a.wgs)), dim3(64 * kWaves), 0, stream, a);
   if (a.whole) return;
   // Contributions to an item, as far as the host can tell. Many: 16 wavefronts to a piece. One sequence of 100000 tokens and 16 heads
-  // over one, 64, 128 and 256 columns, 38, 44 and 45 us, 62, 68 and 59 with 4; 16 of 2000, 256 columns, 8 contributions, 29 and 26.
-  const int64_t tiles = ((int64_t(a.c.max_blocks) << a.c.pshift) + kTile - 1) / kTile, each = a.wgs / items;
-  if ((each < tiles / kWaves ? each : tiles / kWaves) >= 32)
+  // over one, 64, 128 and 256 columns, 38, 44 and 45 us, 62, 68 and 59 with 4; 16 of 2000, 256 columns, 8 contributions, 29 and 26; 32: equal.
+  const int64_t each = a.wgs / items;
+  if ((each < tiles / kWaves ? each : tiles / kWaves) >= 64)
     hipLaunchKernelGGL((k_kv8_tree_join<D, CT, 16>), dim3(unsigned(a.wgs)), dim3(1024), 0, stream, a);
   else
     hipLaunchKernelGGL((k_kv8_tree_join<D, CT, 4>), dim3(unsigned(4 * a.wgs)), dim3(256), 0, stream, a);
 }
 
 // Which kernel, by columns of a sequence and cached head (their mean: only the device knows each) and by the table's length,
-// which bounds the contexts. Graph-timed, us, 16 columns at a time / 64 a workgroup / 128 a workgroup:
-//   Long tables, heads of 128 over 8: 4 sequences of 8192 tokens, 16, 32, 48, 64, 96, 128 columns 22, 23, 44, 32, 47, 51 / 24, 27,
-//   29, 30, 41, 44 / 31, 31, 37, 37, 40, 43; 2 of 32768 35, 34, 68, 52, 76, 89 / 36, 43, 45, 49, 75, 78 / 46, 45, 57, 56, 60, 65.
-//   Heads of 256, 4 of 4096, 32, 64 columns 35, 41 / 29, 34: 16 at a time decode every code once for one wavefront. 16 columns 33 /
-//   28; 64 of 4000 176 / 250, 256 of 500 161 / 174; 4 columns 169 / 262 and 135 / 173: codes past the caches' ordinary order.
+// which bounds the contexts. Graph-timed, us:
+//   Long tables, 16 columns at a time / 64 a workgroup. Up to 16 columns, the first: every code is decoded once in either, for one
+//   wavefront; one node of 64 heads over 8 on 64 sequences of 4000 tokens 98 / 112, heads of 64 42 / 56 (800 to 4000 tokens). Heads of
+//   256 on middle sizes, whose join has more to add, the second: 16 columns, 4 of 1600 to 8192 tokens, 8 heads, 48 / 36, 32 of 400 to
+//   2048, 2 heads, 36 / 27; 64 of 800 to 4000, 8 heads, 147 / 188; one of 2000 16 / 18.
+//   17 to 32 columns are two tiles, whose codes the first decodes twice: 32 on 64 of 240 to 1200 tokens, 8 heads of 128 50 / 43, of 64
+//   41 / 33; 64 of 800 to 4000, 32 heads 460 / 329, 271 / 219; 8 of 800 to 4096, 8 heads 25 / 26, 20 / 21, 4 of 8192 even 35 / 31.
+//   64 / 128 columns a workgroup, heads of 128 over 8: 4 sequences of 8192 tokens, 64, 96, 128 columns 30, 41, 44 / 37, 40, 43; 2 of
+//   32768 49, 75, 78 / 56, 60, 65.
 //   Tables of up to 15 tiles, whose items are not split (a.whole): 16 at a time where those are at most two a CU: 8 sequences of 900
-//   tokens, 64, 128, 256, 512 columns 13, 18, 33, 60 / 24, 25, 26, 37 / 31, 33, 34, 36; 64 of 300, 16, 32, 64, 128 columns 14, 22, 41,
-//   75 / 15, 17, 20, 33 / 19, 20, 25, 30.
+//   tokens, 64, 128, 256, 512 columns 13, 18, 33, 60 / 24, 25, 26, 37 (64 a workgroup) / 31, 33, 34, 36 (128); 64 of 300, 32, 64, 128
+//   columns 22, 41, 75 / 17, 20, 33 / 20, 25, 30; 256 of 500, 4 columns of heads of 256 135 / 173, 16 columns 161 / 174.
 template <int D>
 void tree_launch(Kv8AttnArgs a, int cus, hipStream_t stream) {
-  const int64_t mean = ceil_div(int64_t(a.c.T) * a.G, a.c.B);
+  const int64_t mean = ceil_div(int64_t(a.c.T) * a.G, a.c.B), tiles = ceil_div(int64_t(a.c.max_blocks) << a.c.pshift, kTile);
   const auto items = [&](int columns) { return int64_t(a.c.B) * ceil_div(mean, columns) * a.c.Hkv; };
   a.chunk_from = INT32_MAX;
-  a.whole = (int64_t(a.c.max_blocks) << a.c.pshift) <= 15 * kTile;
-  if (mean <= 16 || (a.whole ? items(16) <= 2 * cus : D != 256 && mean <= 32)) {
+  a.whole = tiles <= 15;
+  const int64_t steps = items(16) * tiles / (2 * cus);   // of 16 columns and a workgroup, if contexts are as long as the table
+  bool few;
+  if (mean <= 16)
+    few = a.whole || D != 256 || steps < 1 || steps >= 8;
+  else if (a.whole)
+    few = items(16) <= 2 * cus;
+  else
+    few = D != 256 && mean <= 32 && steps < 24;
+  if (few) {
     a.col_shift = 4;
     launch_kv8_tree_few(a, D, cus, stream);
     return;
   }
   a.wgs = D == 256 ? tree_wgs(cus) / 2 : tree_wgs(cus);   // as many as run at a time
   if (mean <= 64 || (a.whole && items(64) <= 2 * cus))
-    many_launch<D, 1>(a, items(64), stream);
+    many_launch<D, 1>(a, items(64), tiles, stream);
   else
-    many_launch<D, most_tiles<D>()>(a, items(64 * most_tiles<D>()), stream);
+    many_launch<D, most_tiles<D>()>(a, items(64 * most_tiles<D>()), tiles, stream);
 }
 
 }  // namespace

@@ -153,7 +153,10 @@ def test_left_out(fb):
     (2, 8, 128, 64, [4, 3], [5000, 1000]), (2, 8, 64, 16, [1, 5], [3000, 1300]),            # two columns tiles or fewer
     (2, 8, 128, 64, [6, 7], [3000, 1200]), (2, 8, 64, 32, [5, 8, 0], [2500, 1100, 40]),     # up to 64 columns
     (8, 8, 128, 16, [5] * 40, [100] * 40), (8, 4, 64, 32, [12] * 39 + [3], [200] * 40),     # short tables, many items
-    (8, 8, 128, 64, [16] * 40, [90] * 40), (8, 16, 64, 16, [9] * 40, [70] * 40), (8, 4, 256, 64, [9] * 40, [120] * 40)])
+    (8, 8, 128, 64, [16] * 40, [90] * 40), (8, 16, 64, 16, [9] * 40, [70] * 40), (8, 4, 256, 64, [9] * 40, [120] * 40),
+    (1, 4, 256, 64, [20], [9000]), (1, 8, 64, 64, [10], [9000]), (1, 8, 64, 32, [6], [9000]), (1, 8, 128, 64, [6], [9000]),   # parts
+    (2, 4, 256, 64, [4] * 3, [5000, 1000, 300]), (8, 4, 256, 64, [3] * 4, [4096, 1000, 20, 3]),     # up to 16 columns of 256
+    (8, 2, 256, 64, [2] * 64, [4100] + [70] * 63), (8, 8, 128, 64, [3] * 40, [3000] + [90] * 39), (8, 8, 64, 64, [3] * 40, [3000] + [90] * 39)])
 def test_large(fb, H, G, D, P, new, ctx):
     """Long histories over many workgroups, many columns, many sequences; the workspace holds NaN where nothing was written."""
     log(f"case tree large H={H} G={G} D={D} new={new[:4]} ctx={ctx[:4]}")
