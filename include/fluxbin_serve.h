@@ -105,8 +105,9 @@ fluxbin_status fluxbin_kv8_keep(const fluxbin_kv8_cache* cache, const fluxbin_kv
  * pages are numbered alike).
  *   pages, page_size  as the caches'.
  *   d_state   int32 [pages + 4], 16-byte aligned, zero-filled at first: [0] a page below which none is free (0 is always
- *             valid), [1] pages that the last call wanted and did not find, [2], [3] the library's, [4 + p] the references of
- *             page p. A caller may raise references of its own, and lower them (a page that gets 0 by that needs [0] = 0).
+ *             valid), [1] pages that the last call wanted and did not find (2^31 - 1 if there were more), [2], [3] the
+ *             library's, [4 + p] the references of page p. A caller may raise references of its own, and lower them (a page
+ *             that gets 0 by that needs [0] = 0).
  * Calls that share a pool must not overlap in time. Free pages are taken lowest number first, in the order of the sequences.
  */
 typedef struct {

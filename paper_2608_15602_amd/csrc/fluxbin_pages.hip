@@ -16,8 +16,9 @@ constexpr int kTake = 1024;   // threads of the workgroup that takes pages
 
 __device__ __forceinline__ bool is_page(int page, int pages) { return page >= 0 && page < pages; }
 
-// Inclusive sums over a workgroup's threads; total in every thread.
-__device__ __forceinline__ int block_sum(int v, int* red, int& total) {
+// Inclusive sums over a workgroup's threads, of up to 2^24 each; total in every thread. Rows may want 2^34 pages together, of a pool
+// of 2^24: the total is whole, and sums are cut off at 2^30, which no place among free pages comes near.
+__device__ __forceinline__ int block_sum(int v, int* red, int64_t& total) {
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -29,8 +30,8 @@ __device__ __forceinline__ int block_sum(int v, int* red, int& total) {
   __syncthreads();
   total = 0;
   for (int w = 0; w < kTake / 64; ++w) {
-    const int s = red[w];
-    if (w < wave) v += s;
+    const int s = red[w];   // of 64 threads: up to 2^30
+    if (w < wave) v = int(uint32_t(v) + uint32_t(s) < (1u << 30) ? uint32_t(v) + uint32_t(s) : 1u << 30);
     total += s;
   }
   return v;
@@ -68,9 +69,9 @@ __device__ __forceinline__ pg_i4 counts_at(const PoolArgs& p, int scan) {
 
 // Takes free pages for the wants of up to kTake rows, in order. scan: the page from which on to look, the same in all threads, with
 // the counts there. Returns how many pages were missing, in all threads.
-__device__ int take(const PoolArgs& p, const Taking& mine, int& scan, pg_i4& counts, TakeLds& s) {
+__device__ int64_t take(const PoolArgs& p, const Taking& mine, int& scan, pg_i4& counts, TakeLds& s) {
   const int tid = int(threadIdx.x);
-  int wanted;
+  int64_t wanted;
   const int upto = block_sum(mine.want, s.red, wanted);
   if (wanted == 0) return 0;
   s.upto[tid] = upto;
@@ -88,14 +89,14 @@ __device__ int take(const PoolArgs& p, const Taking& mine, int& scan, pg_i4& cou
       if (at + i < scan) r[i] = 1;
       free += r[i] <= 0 ? 1 : 0;
     }
-    int found;
+    int64_t found;
     int k = block_sum(free, s.red, found) - free;
     if (tid == 0) s.next = (scan & ~3) + 4 * kTake;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (r[i] <= 0) s.list[k++] = at + i;
     __syncthreads();
-    const int n = found < wanted - done ? found : wanted - done;
+    const int n = int(found < wanted - done ? found : wanted - done);
     for (int f = tid; f < n; f += kTake) {
       int lo = 0, rows = kTake;   // the first row whose sum is above that of the page
       while (rows > 0) {
@@ -144,6 +145,8 @@ __device__ int held_entries(const int32_t* row, int most, int pages) {
   return lo;
 }
 
+__device__ __forceinline__ int counted(int64_t missing) { return missing < INT32_MAX ? int(missing) : INT32_MAX; }
+
 __device__ __forceinline__ int need_entries(const ResizeArgs& a, int b) {
   const int t = a.tokens[b];
   if (t < 0) return -1;
@@ -184,7 +187,8 @@ __global__ void __launch_bounds__(kTake) k_pages_resize(ResizeArgs a) {
   const int tid = int(threadIdx.x), lane = tid & 63, pages = a.pool.pages;
   int32_t* refs = a.pool.state + 4;
   Taking mine = {0, 0, nullptr, nullptr, 0};
-  int scan = 0, missing = 0;
+  int scan = 0;
+  int64_t missing = 0;
   pg_i4 counts = {1, 1, 1, 1};
   if (tid == 0) low = INT32_MAX;
   __syncthreads();
@@ -239,7 +243,7 @@ __global__ void __launch_bounds__(kTake) k_pages_resize(ResizeArgs a) {
   }
   if (tid == 0) {
     a.pool.state[0] = scan;
-    a.pool.state[1] = missing;
+    a.pool.state[1] = counted(missing);
     if (!ONE) a.pool.state[2] = 0;
   }
 }
@@ -274,7 +278,8 @@ __global__ void __launch_bounds__(kTake) k_pages_fork(ForkArgs a) {
   __shared__ TakeLds lds;
   const int tid = int(threadIdx.x), lane = tid & 63, pages = a.pool.pages;
   if (blockIdx.x == 0) {
-    int scan = a.pool.state[0], missing = 0;
+    int scan = a.pool.state[0];
+    int64_t missing = 0;
     scan = scan < 0 ? 0 : scan;
     pg_i4 counts = counts_at(a.pool, scan);
     for (int c0 = 0; c0 < a.C; c0 += kTake) {
@@ -296,7 +301,7 @@ __global__ void __launch_bounds__(kTake) k_pages_fork(ForkArgs a) {
     }
     if (tid == 0) {
       a.pool.state[0] = scan;
-      a.pool.state[1] = missing;
+      a.pool.state[1] = counted(missing);
     }
     return;
   }
