@@ -897,7 +897,8 @@ def _page_table(pool: PagePool, name: str, t):
 
 def fluxbin_pages_resize(pool: PagePool, block_table, tokens, stream=None) -> None:
     """Give every row of block_table (int32 [B, blocks], changed in place; a new one is filled with -1) the pages of its first
-    tokens[b] tokens (int32 [B]; negative: the row stays): entries past them are released, missing ones taken."""
+    tokens[b] tokens (int32 [B]; negative: the row stays): entries past them are released, missing ones taken. A row cut to a
+    length inside a page that other rows hold must not be appended to: fork it at that length and release it instead."""
     B, blocks, stride = _page_table(pool, "block_table", block_table)
     _vector(pool.use, pool.index, "tokens", tokens, B)
     status = pool.use.lib.fluxbin_pages_resize(pool.ref, B, blocks, block_table.data_ptr(), stride, tokens.data_ptr(),
@@ -908,7 +909,7 @@ def fluxbin_pages_resize(pool: PagePool, block_table, tokens, stream=None) -> No
 
 def fluxbin_pages_fork(pool: PagePool, block_table, context, source, child_table, copies=None, stream=None):
     """Make row c of child_table (int32 [C, child_blocks]) that of a copy of sequence source[c] (int32 [C]) of block_table with
-    its context tokens (int32 [B]): full pages are shared, a last partial one is taken anew. Returns copies, int32 [C, 2],
+    its context tokens (int32 [B], all of them or the first): full pages are shared, a last partial one is taken anew. Returns copies, int32 [C, 2],
     (old page, new page) or (-1, -1): what fluxbin_kv8_copy_pages takes, for every layer's cache."""
     use = pool.use
     B, blocks, stride = _page_table(pool, "block_table", block_table)

@@ -362,3 +362,44 @@ def test_parallel_samples(fb):
     s.cached(child, pchild, length)
     fb.fluxbin_pages_resize(s.pool, child, ints([0] * C))
     assert not s.pool.refs.any()
+
+
+def test_cut_into_a_shared_page(fb):
+    """A sample cut back to a length inside a page that its prompt holds too: forked at that length, then appended to with larger
+    scales, it changes nothing of the prompt's, and ends where a fork of the prompt at that length would."""
+    import torch
+    log("case cut into a shared page")
+    s = Loop(fb, 1, 8, 20, 6, seed=43)
+    ints = lambda x: torch.from_numpy(np.ascontiguousarray(x, np.int32)).cuda()
+
+    def append(table, ptable, offs, length, scale):
+        k, v = ((s.rng.standard_normal((offs[-1], s.H, s.D)) * scale).astype(np.float16) for _ in range(2))
+        fb.fluxbin_kv8_append(s.cache, torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda(), ints(offs), ints(length), table)
+        s.plain.append(k, v, offs, length, ptable)
+
+    def fork(table, ptable, context):
+        child, pchild = torch.full((1, 6), -1, dtype=torch.int32, device="cuda"), np.full((1, 6), -1, np.int32)
+        copies = fb.fluxbin_pages_fork(s.pool, table, ints(context), ints([0]), child)
+        fb.fluxbin_kv8_copy_pages(s.cache, copies)
+        for f, t in s.ppool.fork(ptable, context, [0], pchild):
+            if f >= 0:
+                s.plain.codes[:, t], s.plain.scales[:, t] = s.plain.codes[:, f], s.plain.scales[:, f]
+        return child, pchild
+
+    def resize(table, ptable, tokens):
+        fb.fluxbin_pages_resize(s.pool, table, ints(tokens))
+        s.ppool.resize(ptable, tokens)
+
+    resize(s.table, s.ptable, [40])
+    append(s.table, s.ptable, [0, 40], [40], 1.0)
+    prompt = [x.clone() for x in fb.fluxbin_kv8_read(s.cache, ints([0, 40]), ints([40]), s.table, 40)]
+    child, pchild = fork(s.table, s.ptable, [40])
+    cut, pcut = fork(child, pchild, [20])
+    resize(child, pchild, [0])
+    resize(cut, pcut, [27])
+    append(cut, pcut, [0, 7], [27], 30.0)
+    assert np.array_equal(cut.cpu().numpy(), pcut) and np.array_equal(s.pool.refs.cpu().numpy(), s.ppool.refs)
+    assert s.ppool.refs[pcut[0, 0]] == 2 and s.ppool.refs[pcut[0, 1]] == 1
+    s.cached(cut, pcut, np.array([27]))
+    now = fb.fluxbin_kv8_read(s.cache, ints([0, 40]), ints([40]), s.table, 40)
+    assert all(torch.equal(x, y) for x, y in zip(prompt, now))
