@@ -92,6 +92,14 @@ def test_many_rows(fb, D, Hq, Hk, inter):
     Case(fb, T, Hq, Hk, D, D, inter, seed=5).run()
 
 
+@pytest.mark.parametrize("D,Hq,Hk,inter,R", [(64, 6, 2, True, 32), (256, 4, 2, False, 192)])
+def test_many_rows_partly_rotated(fb, D, Hq, Hk, inter, R):
+    """Streamed outputs of which elements are not rotated, in the forms that whole heads do not take."""
+    T = (32 << 20) // (2 * (Hq + Hk) * D) + 3
+    log(f"case rotate T={T} D={D} R={R}")
+    Case(fb, T, Hq, Hk, D, R, inter, seed=11).run()
+
+
 def test_far_and_odd_positions(fb):
     """Positions up to 2^31 - 1, negative ones, and a magnitude."""
     log("case rotate far")

@@ -170,6 +170,23 @@ def test_large(fb, H, G, D, P, new, ctx):
     s.verify(new, G, ws=ws, window=60)
 
 
+@pytest.mark.parametrize("H,G,D,P,new,ctx", [
+    (1, 8, 64, 64, [6, 7], [17000, 900]), (1, 8, 64, 32, [16, 10], [17000, 3000]),          # 64 and 128 columns a workgroup
+    (1, 8, 128, 64, [5, 8], [17000, 16600]), (1, 16, 128, 128, [40], [18000]),
+    (1, 4, 256, 64, [20, 6], [17000, 400]), (2, 4, 256, 32, [3, 4], [17000, 3000])])        # one kernel of 256, up to 16 columns too
+def test_many_parts(fb, H, G, D, P, new, ctx):
+    """Few items of long histories, with a hundred parts and more, which 16 wavefronts join; a window that leaves as many, one
+    that leaves few."""
+    log(f"case tree many parts H={H} G={G} D={D} new={new} ctx={ctx}")
+    s = Trees(fb, len(new), H, D, P, max(ctx), seed=49)
+    s.append([c - n for c, n in zip(ctx, new)])
+    s.append(new)
+    ws = fb.make_kv8_tree_workspace(s.cache, sum(new), len(new), H * G)
+    for window in (0, 16900, 60):
+        ws.fill_(0xFF)
+        assert np.isfinite(s.verify(new, G, ws=ws, window=window)).all()
+
+
 def test_bad_pages_and_lengths(fb):
     log("case tree bad pages")
     s = Trees(fb, 5, 2, 64, 16, 64, seed=11)
@@ -412,6 +429,18 @@ def test_keep_many_sequences(fb, P):
     B = 700
     s = Trees(fb, B, 2, 64, P, P + 60, seed=P)
     s.append(s.rng.integers(0, P, B))
+    new = s.rng.integers(0, 50, B)
+    s.append(new, 2.0, lambda k, v: (k.__imul__(s.rng.random((len(k), 1, 1)).astype(np.float16) * 4)))
+    _keep(s, new, [np.flatnonzero(s.rng.random(n) < 0.4) for n in new])
+    s.check()
+
+
+@pytest.mark.parametrize("D", [128, 256])
+def test_keep_many_sequences_of_larger_heads(fb, D):
+    log(f"case keep of many sequences D={D}")
+    B = 530
+    s = Trees(fb, B, 2, D, 32, 90, seed=D)
+    s.append(s.rng.integers(0, 32, B))
     new = s.rng.integers(0, 50, B)
     s.append(new, 2.0, lambda k, v: (k.__imul__(s.rng.random((len(k), 1, 1)).astype(np.float16) * 4)))
     _keep(s, new, [np.flatnonzero(s.rng.random(n) < 0.4) for n in new])
