@@ -105,10 +105,10 @@ def test_many_rows_and_pages(fb):
         s.check()
 
 
-@pytest.mark.parametrize("B,blocks", [(1024, (1 << 21) + (1 << 15)), (1030, 1 << 22)])
+@pytest.mark.parametrize("B,blocks", [(40, 1 << 20), (1100, 1 << 16), (1024, (1 << 21) + (1 << 15)), (1030, 1 << 22)])
 def test_wants_past_32_bits(fb, B, blocks):
-    """Rows that want 2^31 pages together, and 2^32, up to 1024 rows and more: what there is goes to the first of them, and what
-    is missing counts as 2^31 - 1."""
+    """Rows that want 2^25 pages together, and 2^31, and 2^32, up to 1024 rows and more: what there is goes to the first of them,
+    and what is missing is counted, up to 2^31 - 1."""
     import torch
     log(f"case wants past 32 bits B={B} blocks={blocks}")
     pool = fb.make_page_pool(64, 16)
@@ -116,13 +116,14 @@ def test_wants_past_32_bits(fb, B, blocks):
     table = torch.full((B, blocks), -1, dtype=torch.int32, device="cuda")
     tokens = np.full(B, 2 ** 31 - 1, np.int32)
     tokens[:4] = 40, 0, 16 * 30, -1
-    assert sum(min(-(-int(t) // 16), blocks) for t in tokens[tokens > 0]) > 2 ** 31
+    wanted = sum(min(-(-int(t) // 16), blocks) for t in tokens[tokens > 0])
+    assert wanted > 2 ** 25
     fb.fluxbin_pages_resize(pool, table, torch.from_numpy(tokens).cuda())
     free = [p for p in range(64) if p != 10]
     want = np.full((B, 64), -1, np.int32)
     want[0, :3], want[2, :30], want[4, :30] = free[:3], free[3:33], free[33:]
     assert np.array_equal(table[:, :64].cpu().numpy(), want) and int(table[:, 64:].max()) == -1
-    assert (pool.refs == 1).all() and int(pool.missing) == 2 ** 31 - 1
+    assert (pool.refs == 1).all() and int(pool.missing) == min(wanted - 63, 2 ** 31 - 1)
     fb.fluxbin_pages_resize(pool, table, torch.zeros(B, dtype=torch.int32, device="cuda"))
     assert int(table.max()) == -1 and int(pool.missing) == 0 and pool.refs.nonzero().flatten().tolist() == [10]
     del table
