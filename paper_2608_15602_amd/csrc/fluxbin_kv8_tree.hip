@@ -462,8 +462,11 @@ void many_launch(Kv8AttnArgs a, int64_t items, int64_t tiles, hipStream_t stream
 // which bounds the contexts. Graph-timed, us:
 //   Long tables, 16 columns at a time / 64 a workgroup. Up to 16 columns, the first: every code is decoded once in either, for one
 //   wavefront; one node of 64 heads over 8 on 64 sequences of 4000 tokens 98 / 112, heads of 64 42 / 56 (800 to 4000 tokens). Heads of
-//   256 on middle sizes, whose join has more to add, the second: 16 columns, 4 of 1600 to 8192 tokens, 8 heads, 48 / 36, 32 of 400 to
-//   2048, 2 heads, 36 / 27; 64 of 800 to 4000, 8 heads, 147 / 188; one of 2000 16 / 18.
+//   256 on middle sizes, whose join has more to add, the second. 426 cases of one sequence to 64, even and ragged, mean of the first's
+//   time over the second's by steps (below): 9 to 16 columns, steps 0, 1, 2, 4, 8, 10, 11, 12, 16, 20 and more: 0.92, 0.97, 1.11, 1.31,
+//   1.25, 1.07, 0.93, 1.02, 0.98, 0.78 (4 sequences of 1600 to 8192 tokens, 8 heads 43 / 36; 32 of 400 to 2048, 2 heads 36 / 27; 64 of
+//   800 to 4000, 8 heads 145 / 182; one of 2000 16 / 18; steps of 1 are about even, but one of 16384, 2 heads, 27 / 22); up to 8
+//   columns, steps 1, 2, 3, 4, 7, 8, 10, 16: 0.86, 0.92, 1.06, 1.07, 0.99, 1.02 (even ones 0.9), 0.95, 0.85.
 //   17 to 32 columns are two tiles, whose codes the first decodes twice: 32 on 64 of 240 to 1200 tokens, 8 heads of 128 50 / 43, of 64
 //   41 / 33; 64 of 800 to 4000, 32 heads 460 / 329, 271 / 219; 8 of 800 to 4096, 8 heads 25 / 26, 20 / 21, 4 of 8192 even 35 / 31.
 //   64 / 128 columns a workgroup, heads of 128 over 8: 4 sequences of 8192 tokens, 64, 96, 128 columns 30, 41, 44 / 37, 40, 43; 2 of
@@ -480,7 +483,7 @@ void tree_launch(Kv8AttnArgs a, int cus, hipStream_t stream) {
   const int64_t steps = items(16) * tiles / (2 * cus);   // of 16 columns and a workgroup, if contexts are as long as the table
   bool few;
   if (mean <= 16)
-    few = a.whole || D != 256 || steps < 1 || steps >= 8;
+    few = a.whole || D != 256 || steps < (mean > 8 ? 1 : 3) || steps >= (mean > 8 ? 11 : 8);
   else if (a.whole)
     few = items(16) <= 2 * cus;
   else
