@@ -73,7 +73,9 @@ fluxbin_status fluxbin_tree_masks(int64_t rows, int32_t sequences, const int32_t
  * sequence's first row (j < d_context - n) and, of its n rows, those whose bit is set in the row's mask, at any place in the
  * order. With window > 0 it attends only the last `window` of these (bits at negative positions do not count, positions
  * without a page do). Masks that fluxbin_tree_masks makes of a chain are the causal mask. A row that attends nothing is 0.
- * Precision, strides and argument checks as fluxbin_kv8_attention's; the workspace is this call's own size.
+ * Precision, strides and argument checks as fluxbin_kv8_attention's; the workspace is this call's own size, whose bytes go by
+ * the cache's head_dim and the device alone. How work is split goes by max_blocks, since lengths are read on the device: for contexts
+ * of up to 900 tokens or so, a table no wider than they need (a view of its first columns) takes down to half of the time.
  */
 fluxbin_status fluxbin_kv8_tree_workspace_query(const fluxbin_kv8_cache* cache, int64_t rows, int32_t sequences,
                                                 int32_t q_heads, size_t* bytes);

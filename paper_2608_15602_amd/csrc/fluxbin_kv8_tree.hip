@@ -43,7 +43,8 @@ __device__ __forceinline__ void interleave() {
 
 // Workgroup: a share of the units, as k_kv8_attention's; an item is 64 CT columns of a sequence and cached head. A tile's decoding,
 // scores, weights and output are one barrier apart: the next tile is decoded, from requests sent a tile before, beside the last
-// products, and the weights of the tile's second half beside those of its first. CT = 2 halves the traffic from LDS for a column;
+// products, and the weights of the tile's second half beside those of its first; the row sums' 16 CT fused steps, two chains, come
+// behind the last product, where the compiler puts them and no product runs beside them. CT = 2 halves the traffic from LDS for a column;
 // its 256 registers allow two workgroups per CU, as do 64 KB of LDS (D = 256: 128 KB, one).
 // Heads of 128, 64 over 8: trees of 48 to 64 rows on 8 sequences of 256 to 8192 tokens 94 us a call, 80 of them here and 13 the join
 // (52 MB of partial results), 428 TFLOP/s by the formula's products, 640 by those done; 13 to 16 rows on 50000 and 65536 tokens
@@ -276,7 +277,7 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) k_kv8_tree(Kv8A
       auto weights = [&](int h, int n) __attribute__((always_inline)) {   // two of a half's 8 CT of a lane
         const int c = n >> 2, j = (n >> 1) & 1, i = 2 * (n & 1);
         const float p0 = __builtin_amdgcn_exp2f(sc[c][2 * h + j][i]), p1 = __builtin_amdgcn_exp2f(sc[c][2 * h + j][i + 1]);
-        // p before it is rounded: a weight on values of a tiny scale may be lost in p, but not in the sum
+        // p before it is rounded: a weight on values of a tiny scale may be lost in p, but not in the sum (built behind the products)
         sum[c] = __builtin_fmaf(p0, rj[2 * h + j], sum[c]);
         sum[c] = __builtin_fmaf(p1, rj[2 * h + j], sum[c]);
         // the first number cut off (a pair an instruction), the second the rest of it, rounded: 21 bits
@@ -459,7 +460,10 @@ void many_launch(Kv8AttnArgs a, int64_t items, int64_t tiles, hipStream_t stream
 }
 
 // Which kernel, by columns of a sequence and cached head (their mean: only the device knows each) and by the table's length,
-// which bounds the contexts. Graph-timed, us:
+// which bounds the contexts. Where it is far longer than they are, short items are split and joined all the same (table four times
+// as long and more, heads of 128: one sequence of 200 tokens, 8 columns 7.4 -> 9.7, 64 columns 8 -> 15; 8 of 900, 64 columns 12.5 -> 21;
+// 64 of 300, 32 columns 15 -> 28, 128 columns 28 -> 41; 8 of 8192 and 64 of 2000 as long as before), and the steps below are more than
+// there are (heads of 256, 32 of 400 to 2048, 16 columns 27 -> 36). Graph-timed, us:
 //   Long tables, 16 columns at a time / 64 a workgroup. Up to 16 columns, the first: every code is decoded once in either, for one
 //   wavefront; one node of 64 heads over 8 on 64 sequences of 4000 tokens 98 / 112, heads of 64 42 / 56 (800 to 4000 tokens). Heads of
 //   256 on middle sizes, whose join has more to add, the second. 426 cases of one sequence to 64, even and ragged, mean of the first's
