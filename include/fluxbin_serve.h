@@ -127,7 +127,8 @@ typedef struct {
  * Gives every row of a block table the pages of its first d_tokens[b] tokens (int32 [sequences]; a row with a negative number
  * stays as it is): entries past the last are released (-1), then missing ones taken, as far as the table has columns and the
  * pool has free pages. A last page that the tokens fill partly stays the row's, also where other rows hold it (see above for
- * what then may not be stored there). d_block_table is read and written, int32 [sequences][max_blocks], row stride block_table_stride.
+ * what then may not be stored there). d_block_table is read and written, int32 [sequences][max_blocks], row stride
+ * block_table_stride.
  */
 fluxbin_status fluxbin_pages_resize(const fluxbin_page_pool* pool, int32_t sequences, int32_t max_blocks,
                                     int32_t* d_block_table, int64_t block_table_stride, const int32_t* d_tokens,
@@ -138,8 +139,9 @@ fluxbin_status fluxbin_pages_resize(const fluxbin_page_pool* pool, int32_t seque
  * sequence d_source[c] (int32 [children]) of the table (lengths in d_context, int32 [sequences]). Pages that the tokens fill
  * are shared and get a reference; a last page that they fill partly is taken from the pool, and d_copies[c] (int32
  * [children][2]) is (old page, new page) for fluxbin_kv8_copy_pages, of every layer's cache, otherwise (-1, -1). The rest of
- * the row becomes -1, with the partly filled page where the pool had none: such a row lacks its last tokens. The child table's old entries are overwritten, not released (resize them to 0 first). A source outside
- * [0, sequences) gives an empty row; tokens past child_blocks are cut off.
+ * the row becomes -1, with the partly filled page where the pool had none: such a row lacks its last tokens. The child
+ * table's old entries are overwritten, not released (resize them to 0 first). A source outside [0, sequences) gives an empty
+ * row; tokens past child_blocks are cut off.
  */
 fluxbin_status fluxbin_pages_fork(const fluxbin_page_pool* pool, int32_t sequences, int32_t max_blocks,
                                   const int32_t* d_block_table, int64_t block_table_stride, const int32_t* d_context,

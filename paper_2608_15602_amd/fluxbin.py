@@ -909,8 +909,8 @@ def fluxbin_pages_resize(pool: PagePool, block_table, tokens, stream=None) -> No
 
 def fluxbin_pages_fork(pool: PagePool, block_table, context, source, child_table, copies=None, stream=None):
     """Make row c of child_table (int32 [C, child_blocks]) that of a copy of sequence source[c] (int32 [C]) of block_table with
-    its context tokens (int32 [B], all of them or the first): full pages are shared, a last partial one is taken anew. Returns copies, int32 [C, 2],
-    (old page, new page) or (-1, -1): what fluxbin_kv8_copy_pages takes, for every layer's cache."""
+    its context tokens (int32 [B], all of them or the first): full pages are shared, a last partial one is taken anew. Returns
+    copies, int32 [C, 2], (old page, new page) or (-1, -1): what fluxbin_kv8_copy_pages takes, for every layer's cache."""
     use = pool.use
     B, blocks, stride = _page_table(pool, "block_table", block_table)
     C, child_blocks, child_stride = _page_table(pool, "child_table", child_table)
